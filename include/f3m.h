@@ -281,6 +281,115 @@ f3m_status direct_kmvm_xy_rows_f64(const float *X, int64_t nx, const float *Y, i
 f3m_status f3m_cg_solve(f3m_plan_t *plan, float lambda, const float *b, float *x, int max_iter, float tol,
                         int *iters_host, float *history_host, void *stream);
 
+/* ---- row-normalised products (attention) ----
+ *
+ * direct_kmvm_xy with another kernel, each row divided by its sum and a vector per source instead of a number:
+ *   o_i = sum_j w_ij v_j,   w_ij = exp(scale q_i.k_j) / sum_j' exp(scale q_i.k_j')   over the visible j, j'
+ * (with k = (y, -|y|^2/2) and q = (x, 1) and scale 1/lengthscale^2 it is the smoother K(X,Y) V / K(X,Y) 1 of the
+ * Gaussian kernel).  In 16 bits with fp32 sums, on the matrix cores.
+ *
+ * Heads: q has `heads` heads, k and v kv_heads, heads = g kv_heads; head h of q reads head h / g.
+ * Sequences: rows of all sequences lie behind one another; sequence b has rows q_offsets[b] .. q_offsets[b+1] - 1 of q
+ * (nq of them) and k_offsets[b] .. of k and v (nk).  Token i of a sequence stands at position nk - nq + i: the last
+ * query at the last key.  Lengths of 0 are allowed, and differ from sequence to sequence.
+ * Visible to the token at position p: with causal = 0 all keys of its sequence; else the keys j <= p, with window > 0
+ * of those the last `window` (j > p - window) and the first `sinks` keys of the sequence.  A token that sees no key
+ * (p < 0) gets o = 0 and lse = -inf, and adds nothing to the gradients.  What hidden keys hold (NaN, infinities)
+ * reaches no token, nor do hidden tokens' values reach a key's gradients.  A NaN or infinity in a visible row of v makes at
+ * least the same elements of o NaN or infinite, one in k, q or dout all that depends on the pair.
+ * Offsets and lengths are read on the device and not checked by the host: such as lie outside the tensors or fall are
+ * cut to what exists, no access leaves the tensors.
+ * Limits: head_dim a multiple of 8 up to 128; data 16-byte aligned, strides multiples of 8 values; fewer than
+ * 2^31 - 65536 rows.
+ * Every call is asynchronous on `stream` and allocates nothing; the caller brings the workspace (the *_workspace calls
+ * say how many bytes) and gives each call that may run at the same time its own.  Any call may be captured into a HIP
+ * graph.  Sums are made in a fixed order: results repeat bit for bit.
+ */
+typedef enum { F3M_BF16 = 0, F3M_F16 = 1, F3M_E4M3 = 2 } f3m_dtype;
+
+/* a tensor of rows x heads x head_dim: strides in values between rows and between heads, head_dim contiguous */
+typedef struct {
+    void *data;
+    int64_t row, head;
+} f3m_rows;
+
+typedef struct {
+    int32_t dtype;             /* F3M_BF16 or F3M_F16, of q, k, v and the results */
+    int32_t batch;             /* sequences, >= 0 */
+    int32_t heads, kv_heads, head_dim;
+    int32_t causal, window, sinks; /* window: 0 = none; window and sinks need causal */
+    float scale;               /* finite and > 0 */
+    int32_t max_q, max_k;      /* the longest sequence's nq and nk, or more (the host cannot see the offsets).  Tokens of a
+                                  sequence from max_q on, and keys' gradients from max_k on, are not computed; with keys past
+                                  max_k the results of that sequence are not defined */
+    int64_t total_q, total_k;  /* rows of q; rows of k and v.  Rows outside all sequences are left as they are */
+    const int32_t *q_offsets, *k_offsets; /* device, batch + 1 each; both NULL with batch = 1: one sequence of all rows */
+    f3m_rows q, k, v;          /* device; a stride may be 0 (a row or head that all share) */
+} f3m_attention_args;
+
+/* bytes of workspace for f3m_attention (cache NULL) or f3m_cache_attention with these sizes, and for
+ * f3m_attention_grad; negative: -f3m_status */
+int64_t f3m_attention_workspace(const f3m_attention_args *args);
+int64_t f3m_attention_grad_workspace(const f3m_attention_args *args);
+
+/*
+ * f3m_attention - o and lse[row * heads + head] = log sum_j exp(scale q.k_j) (fp32).  The weights are rounded to
+ * dtype for the product with v (half a step each, 2^-9 in bf16, 2^-12 in fp16), o once more at the end.
+ */
+f3m_status f3m_attention(const f3m_attention_args *args, const f3m_rows *out, float *lse, void *workspace,
+                         int64_t workspace_bytes, void *stream);
+
+/*
+ * f3m_attention_grad - the gradients of a loss whose gradient with respect to o is dout: dq, dk, dv (overwritten, summed
+ * over the heads that share a key head), from the out and lse of f3m_attention with the same arguments.  lse carries no
+ * gradient.  The weights and their gradients are rounded to dtype for the products; in fp16 after scaling by powers of
+ * two, so that small gradients keep their bits.
+ */
+f3m_status f3m_attention_grad(const f3m_attention_args *args, const f3m_rows *dout, const f3m_rows *out, const float *lse,
+                              const f3m_rows *dq, const f3m_rows *dk, const f3m_rows *dv, void *workspace,
+                              int64_t workspace_bytes, void *stream);
+
+/*
+ * A cache of k and v in pages, for sequences that grow.  Device memory of the caller, contiguous:
+ *   k, v          pages x kv_heads x page_size x head_dim values of type `held`
+ *   k_exp, v_exp  pages x kv_heads x page_size bytes, with F3M_E4M3 only (else NULL)
+ * Slot s is row s % page_size of page s / page_size.  held = F3M_E4M3: a row's values are code * 2^(byte - 127); the byte is the
+ * least that keeps the row's largest finite value within 448, from 1 to 254, so that writing rounds once, to e4m3, and
+ * reading is exact (in fp16, values beyond its range become infinite).  Infinities and NaN are kept as NaN.  head_dim is a
+ * multiple of 16 then.  page_size is a power of two from 8 to 1024.
+ */
+typedef struct {
+    int32_t held;              /* F3M_BF16, F3M_F16 or F3M_E4M3 */
+    int32_t kv_heads, head_dim, page_size;
+    int64_t pages;             /* pages * page_size below 2^40 */
+    void *k, *v;
+    uint8_t *k_exp, *v_exp;
+} f3m_cache;
+
+/*
+ * f3m_cache_write - rows k, v (tokens x kv_heads x head_dim of dtype F3M_BF16 or F3M_F16; a 16-bit cache holds the same
+ * type) to slots[tokens] (device).  A slot below 0 or past the last page is skipped.  Slots of one call differ: of a slot given twice
+ * the contents are not defined.
+ * f3m_cache_read - the reverse, with zeros for such slots.
+ */
+f3m_status f3m_cache_write(const f3m_cache *cache, int dtype, const f3m_rows *k, const f3m_rows *v, const int64_t *slots,
+                           int64_t tokens, void *stream);
+f3m_status f3m_cache_read(const f3m_cache *cache, int dtype, const f3m_rows *k, const f3m_rows *v, const int64_t *slots,
+                          int64_t tokens, void *stream);
+
+/*
+ * f3m_cache_attention - f3m_attention of new tokens (q) over the sequences of a cache, which hold the new tokens' own
+ * keys already.  Key j of sequence b is row j % page_size of page table[b * table_row + j / page_size], j < lengths[b].
+ *   args       as for f3m_attention; k, v, k_offsets and total_k are not read, dtype is that of q and out (a 16-bit cache
+ *              holds the same)
+ *   table      device, batch rows of table_cols page numbers; entries that no key lies in may hold anything.  Keys in a page
+ *              outside 0 .. pages - 1 are hidden.
+ *   lengths    device int32[batch], at most table_cols * page_size (cut to it)
+ */
+f3m_status f3m_cache_attention(const f3m_cache *cache, const f3m_attention_args *args, const int32_t *table, int64_t table_row,
+                               int32_t table_cols, const int32_t *lengths, const f3m_rows *out, float *lse, void *workspace,
+                               int64_t workspace_bytes, void *stream);
+
 /* Destroys the plan (NULL is allowed); waits for the device first.  Its device buffers go back to the
  * library's memory pool, where the next plan finds them again (building plan after plan then costs no
  * hipMalloc / hipFree); the pool keeps at most 96 GiB and gives the rest back to the device at once. */

@@ -4,6 +4,7 @@
 #include <cstring>
 #include <new>
 
+#include "attend.h"
 #include "plan.h"
 
 namespace {
@@ -55,6 +56,110 @@ template <class T>
 void copy_to_host(T *dst, const T *src, size_t count) {
     if (count == 0) return;
     F3M_HIP(hipMemcpy(dst, src, count * sizeof(T), hipMemcpyDeviceToHost));
+}
+
+// ---- attention ----
+
+f3m::Rows rows_of(const f3m_rows &r) { return {(char *)r.data, r.row, r.head}; }
+
+// `paged`: k, v, k_offsets and total_k are not read
+f3m_status check_attention(const f3m_attention_args *p, bool paged = false) {
+    if (!p) return set_error(F3M_ERR_INVALID_ARG, "args is null");
+    if (p->dtype != F3M_BF16 && p->dtype != F3M_F16) return set_error(F3M_ERR_INVALID_ARG, "dtype must be F3M_BF16 or F3M_F16");
+    if (p->heads < 1 || p->kv_heads < 1 || p->heads % p->kv_heads) return set_error(F3M_ERR_INVALID_ARG, "heads must be a positive multiple of kv_heads");
+    if (p->head_dim < 8 || p->head_dim % 8) return set_error(F3M_ERR_INVALID_ARG, "head_dim must be a positive multiple of 8");
+    if (p->head_dim > 128) return set_error(F3M_ERR_UNSUPPORTED, "head_dim above 128 is not supported");
+    if (p->batch < 0 || p->max_q < 0 || p->max_k < 0 || p->total_q < 0 || p->total_k < 0)
+        return set_error(F3M_ERR_INVALID_ARG, "batch, max_q, max_k, total_q and total_k must be >= 0");
+    if (p->window < 0 || p->sinks < 0) return set_error(F3M_ERR_INVALID_ARG, "window and sinks must be >= 0");
+    if (p->window && !p->causal) return set_error(F3M_ERR_INVALID_ARG, "a window needs causal order");
+    if (p->sinks && !p->window) return set_error(F3M_ERR_INVALID_ARG, "sinks need a window");
+    if (!finite_pos(p->scale)) return set_error(F3M_ERR_INVALID_ARG, "scale must be finite and > 0");
+    if (!paged && (!p->q_offsets != !p->k_offsets)) return set_error(F3M_ERR_INVALID_ARG, "q_offsets and k_offsets are given both or neither");
+    if (!p->q_offsets && p->batch != 1) return set_error(F3M_ERR_INVALID_ARG, "without offsets batch is 1");
+    constexpr int64_t most = ((int64_t)1 << 31) - 65536;   // indices of a tile past the last row stay ints
+    if (p->total_q >= most || p->total_k >= most || (int64_t)p->max_q * (p->heads / p->kv_heads) >= most ||
+        (int64_t)p->batch * p->kv_heads >= ((int64_t)1 << 24))
+        return set_error(F3M_ERR_UNSUPPORTED, "rows (times heads to a key head) must stay below 2^31 - 65536, batch * kv_heads below 2^24");
+    return F3M_OK;
+}
+
+f3m_status check_rows(const f3m_rows &r, int64_t rows, const char *name) {
+    (void)rows;
+    if (!r.data) return set_error(F3M_ERR_INVALID_ARG, std::string(name) + " is null");
+    if ((uintptr_t)r.data % 16 || r.row % 8 || r.head % 8 || r.row < 0 || r.head < 0)
+        return set_error(F3M_ERR_INVALID_ARG, std::string(name) + ": data must be 16-byte aligned, strides multiples of 8 values and >= 0");
+    return F3M_OK;
+}
+
+// results do not overlap themselves: one stride steps over all that the other spans
+f3m_status check_result(const f3m_rows *r, const f3m_attention_args &p, int64_t rows, int heads, const char *name) {
+    if (!r) return set_error(F3M_ERR_INVALID_ARG, std::string(name) + " is null");
+    f3m_status st = check_rows(*r, rows, name);
+    if (st != F3M_OK) return st;
+    const bool by_row = (heads == 1 || r->head >= p.head_dim) && (rows == 1 || r->row >= (heads - 1) * (heads == 1 ? 0 : r->head) + p.head_dim);
+    const bool by_head = (rows == 1 || r->row >= p.head_dim) && (heads == 1 || r->head >= (rows - 1) * (rows == 1 ? 0 : r->row) + p.head_dim);
+    if (!by_row && !by_head) return set_error(F3M_ERR_INVALID_ARG, std::string(name) + ": rows that are written must not overlap");
+    return F3M_OK;
+}
+
+f3m_status check_workspace(const void *p, int64_t bytes, int64_t needed) {
+    if (needed > 0 && !p) return set_error(F3M_ERR_INVALID_ARG, "workspace is null");
+    if (bytes < needed) return set_error(F3M_ERR_INVALID_ARG, "workspace is too small");
+    if ((uintptr_t)p % 16) return set_error(F3M_ERR_INVALID_ARG, "workspace must be 16-byte aligned");
+    return F3M_OK;
+}
+
+f3m_status check_cache(const f3m_cache *c) {
+    if (!c) return set_error(F3M_ERR_INVALID_ARG, "cache is null");
+    if (c->held != F3M_BF16 && c->held != F3M_F16 && c->held != F3M_E4M3) return set_error(F3M_ERR_INVALID_ARG, "held must be F3M_BF16, F3M_F16 or F3M_E4M3");
+    if (c->kv_heads < 1 || c->head_dim < 8 || c->head_dim % 8) return set_error(F3M_ERR_INVALID_ARG, "kv_heads must be positive, head_dim a positive multiple of 8");
+    if (c->held == F3M_E4M3 && c->head_dim % 16) return set_error(F3M_ERR_UNSUPPORTED, "8-bit caches need a head_dim that is a multiple of 16");
+    if (c->head_dim > 128) return set_error(F3M_ERR_UNSUPPORTED, "head_dim above 128 is not supported");
+    if (c->page_size < 8 || c->page_size > 1024 || (c->page_size & (c->page_size - 1)))
+        return set_error(F3M_ERR_INVALID_ARG, "page_size must be a power of two from 8 to 1024");
+    if (c->pages < 0 || c->pages >= ((int64_t)1 << 40) / c->page_size) return set_error(F3M_ERR_INVALID_ARG, "pages * page_size must be in [0, 2^40)");
+    if (c->pages > 0) {
+        if (!c->k || !c->v) return set_error(F3M_ERR_INVALID_ARG, "k or v of the cache is null");
+        if ((uintptr_t)c->k % 16 || (uintptr_t)c->v % 16) return set_error(F3M_ERR_INVALID_ARG, "the cache's data must be 16-byte aligned");
+        if (c->held == F3M_E4M3 && (!c->k_exp || !c->v_exp)) return set_error(F3M_ERR_INVALID_ARG, "an 8-bit cache needs k_exp and v_exp");
+    }
+    return F3M_OK;
+}
+
+f3m_status check_cache_rows(const f3m_cache *c, int dtype, const f3m_rows *k, const f3m_rows *v, const int64_t *slots, int64_t tokens) {
+    f3m_status st = check_cache(c);
+    if (st != F3M_OK) return st;
+    if (dtype != F3M_BF16 && dtype != F3M_F16) return set_error(F3M_ERR_INVALID_ARG, "dtype must be F3M_BF16 or F3M_F16");
+    if (c->held != F3M_E4M3 && c->held != dtype) return set_error(F3M_ERR_INVALID_ARG, "a 16-bit cache holds the type of the rows");
+    if (tokens < 0) return set_error(F3M_ERR_INVALID_ARG, "tokens must be >= 0");
+    if (tokens == 0) return F3M_OK;
+    if (!k || !v || !slots) return set_error(F3M_ERR_INVALID_ARG, "k, v or slots is null");
+    st = check_rows(*k, tokens, "k");
+    return st != F3M_OK ? st : check_rows(*v, tokens, "v");
+}
+
+f3m::AttendArgs attend_args(const f3m_attention_args &p) {
+    f3m::AttendArgs a = {};
+    a.batch = p.batch;
+    a.heads = p.heads;
+    a.kv_heads = p.kv_heads;
+    a.group = p.heads / p.kv_heads;
+    a.dim = p.head_dim;
+    a.causal = p.causal != 0;
+    a.window = p.window;
+    a.sinks = p.window ? p.sinks : 0;
+    a.scale = p.scale;
+    a.total_q = p.total_q;
+    a.total_k = p.total_k;
+    a.max_q = (int)std::min<int64_t>(p.max_q, p.total_q);
+    a.q_offsets = p.q_offsets;
+    a.k_offsets = p.k_offsets;
+    a.q = rows_of(p.q);
+    a.k = rows_of(p.k);
+    a.v = rows_of(p.v);
+    a.groups = p.batch * p.kv_heads;
+    return a;
 }
 
 }  // namespace
@@ -240,6 +345,123 @@ f3m_status f3m_cg_solve(f3m_plan_t *plan, float lambda, const float *b, float *x
     if (!b || !x) return set_error(F3M_ERR_INVALID_ARG, "b or x is null");
     if (b == x) return set_error(F3M_ERR_INVALID_ARG, "b and x must not overlap");
     return guarded([&] { f3m::run_cg(*plan, lambda, b, x, max_iter, tol, iters_host, history_host, (hipStream_t)stream); });
+}
+
+int64_t f3m_attention_workspace(const f3m_attention_args *args) {
+    f3m_status st = check_attention(args, true);   // also asked for calls over a cache
+    return st != F3M_OK ? -(int64_t)st : f3m::attend_workspace(attend_args(*args), args->max_k);
+}
+
+int64_t f3m_attention_grad_workspace(const f3m_attention_args *args) {
+    f3m_status st = check_attention(args);
+    return st != F3M_OK ? -(int64_t)st : f3m::attend_grad_workspace(attend_args(*args));
+}
+
+f3m_status f3m_attention(const f3m_attention_args *args, const f3m_rows *out, float *lse, void *workspace, int64_t workspace_bytes,
+                         void *stream) {
+    f3m_status st = check_attention(args);
+    if (st == F3M_OK && args->total_q > 0) {
+        st = check_rows(args->q, args->total_q, "q");
+        if (st == F3M_OK && args->total_k > 0) st = check_rows(args->k, args->total_k, "k");
+        if (st == F3M_OK && args->total_k > 0) st = check_rows(args->v, args->total_k, "v");
+        if (st == F3M_OK) st = check_result(out, *args, args->total_q, args->heads, "out");
+        if (st == F3M_OK && !lse) st = set_error(F3M_ERR_INVALID_ARG, "lse is null");
+    }
+    if (st != F3M_OK || args->total_q == 0 || args->batch == 0) return st;
+    f3m::AttendArgs a = attend_args(*args);
+    st = check_workspace(workspace, workspace_bytes, f3m::attend_workspace(a, args->max_k));
+    if (st != F3M_OK) return st;
+    a.out = rows_of(*out);
+    a.lse = lse;
+    return guarded([&] { f3m::run_attend(a, args->max_k, args->dtype == F3M_F16, false, workspace, (hipStream_t)stream); });
+}
+
+f3m_status f3m_attention_grad(const f3m_attention_args *args, const f3m_rows *dout, const f3m_rows *out, const float *lse,
+                              const f3m_rows *dq, const f3m_rows *dk, const f3m_rows *dv, void *workspace, int64_t workspace_bytes,
+                              void *stream) {
+    f3m_status st = check_attention(args);
+    if (st != F3M_OK || args->batch == 0) return st;
+    if (args->total_q > 0) {
+        if (!dout || !out || !lse) return set_error(F3M_ERR_INVALID_ARG, "dout, out or lse is null");
+        st = check_rows(args->q, args->total_q, "q");
+        if (st == F3M_OK) st = check_rows(*dout, args->total_q, "dout");
+        if (st == F3M_OK) st = check_rows(*out, args->total_q, "out");
+        if (st == F3M_OK) st = check_result(dq, *args, args->total_q, args->heads, "dq");
+    }
+    if (st == F3M_OK && args->total_k > 0) {
+        st = check_rows(args->k, args->total_k, "k");
+        if (st == F3M_OK) st = check_rows(args->v, args->total_k, "v");
+        if (st == F3M_OK) st = check_result(dk, *args, args->total_k, args->kv_heads, "dk");
+        if (st == F3M_OK) st = check_result(dv, *args, args->total_k, args->kv_heads, "dv");
+    }
+    if (st != F3M_OK) return st;
+    f3m::AttendArgs a = attend_args(*args);
+    st = check_workspace(workspace, workspace_bytes, f3m::attend_grad_workspace(a));
+    if (st != F3M_OK) return st;
+    if (args->total_q > 0) {
+        a.dout = rows_of(*dout);
+        a.out = rows_of(*out);
+        a.lse = const_cast<float *>(lse);
+        a.dq = rows_of(*dq);
+    }
+    if (args->total_k > 0) {
+        a.dk = rows_of(*dk);
+        a.dv = rows_of(*dv);
+    }
+    return guarded([&] { f3m::run_attend_grad(a, args->max_k, args->dtype == F3M_F16, workspace, (hipStream_t)stream); });
+}
+
+f3m_status f3m_cache_write(const f3m_cache *cache, int dtype, const f3m_rows *k, const f3m_rows *v, const int64_t *slots, int64_t tokens,
+                           void *stream) {
+    f3m_status st = check_cache_rows(cache, dtype, k, v, slots, tokens);
+    if (st != F3M_OK || tokens == 0) return st;
+    return guarded([&] { f3m::run_cache_rows(*cache, dtype == F3M_F16, slots, tokens, *k, *v, true, (hipStream_t)stream); });
+}
+
+f3m_status f3m_cache_read(const f3m_cache *cache, int dtype, const f3m_rows *k, const f3m_rows *v, const int64_t *slots, int64_t tokens,
+                          void *stream) {
+    f3m_status st = check_cache_rows(cache, dtype, k, v, slots, tokens);
+    if (st != F3M_OK || tokens == 0) return st;
+    if (k->head < cache->head_dim || k->row < cache->head_dim || v->head < cache->head_dim || v->row < cache->head_dim)
+        return set_error(F3M_ERR_INVALID_ARG, "rows that are written must not overlap");
+    return guarded([&] { f3m::run_cache_rows(*cache, dtype == F3M_F16, slots, tokens, *k, *v, false, (hipStream_t)stream); });
+}
+
+f3m_status f3m_cache_attention(const f3m_cache *cache, const f3m_attention_args *args, const int32_t *table, int64_t table_row,
+                               int32_t table_cols, const int32_t *lengths, const f3m_rows *out, float *lse, void *workspace,
+                               int64_t workspace_bytes, void *stream) {
+    f3m_status st = check_attention(args, true);
+    if (st == F3M_OK) st = check_cache(cache);
+    if (st != F3M_OK) return st;
+    if (cache->kv_heads != args->kv_heads || cache->head_dim != args->head_dim)
+        return set_error(F3M_ERR_INVALID_ARG, "the cache has another number of heads or another head_dim");
+    if (cache->held != F3M_E4M3 && cache->held != args->dtype)
+        return set_error(F3M_ERR_INVALID_ARG, "a 16-bit cache holds the type of q");
+    if (table_cols < 0 || table_row < table_cols) return set_error(F3M_ERR_INVALID_ARG, "table_row must be >= table_cols >= 0");
+    if ((int64_t)table_cols * cache->page_size >= ((int64_t)1 << 31) - 65536)
+        return set_error(F3M_ERR_UNSUPPORTED, "table_cols * page_size must be below 2^31 - 65536");
+    if (args->total_q == 0 || args->batch == 0) return F3M_OK;
+    if (!lengths || (table_cols > 0 && !table)) return set_error(F3M_ERR_INVALID_ARG, "table or lengths is null");
+    st = check_rows(args->q, args->total_q, "q");
+    if (st == F3M_OK) st = check_result(out, *args, args->total_q, args->heads, "out");
+    if (st != F3M_OK) return st;
+    if (!lse) return set_error(F3M_ERR_INVALID_ARG, "lse is null");
+    f3m::AttendArgs a = attend_args(*args);
+    st = check_workspace(workspace, workspace_bytes, f3m::attend_workspace(a, args->max_k));
+    if (st != F3M_OK) return st;
+    a.out = rows_of(*out);
+    a.lse = lse;
+    a.k = {(char *)cache->k, 0, 0};
+    a.v = {(char *)cache->v, 0, 0};
+    a.k_exp = cache->k_exp;
+    a.v_exp = cache->v_exp;
+    a.table = table_cols > 0 && cache->pages > 0 ? table : (const int32_t *)lengths;   // no page: every length is cut to 0
+    a.table_row = table_row;
+    a.table_cols = cache->pages > 0 ? table_cols : 0;
+    a.pages = cache->pages;
+    a.page_shift = __builtin_ctz((unsigned)cache->page_size);
+    a.lengths = lengths;
+    return guarded([&] { f3m::run_attend(a, args->max_k, args->dtype == F3M_F16, cache->held == F3M_E4M3, workspace, (hipStream_t)stream); });
 }
 
 int64_t f3m_trim_memory(void) {

@@ -1,0 +1,275 @@
+// Row-normalised products (attention): what the kernels of attend.hip, attend_grad.hip and attend_few.hip share.
+//
+// Every product of a 32 x 32 block runs on v_mfma_f32_32x32x16 (fp32 sums).  Lane l of a wave has the operand values
+//   A[l % 32][8 (l / 32) + j],  B[8 (l / 32) + j][l % 32],  j = 0..7
+// and the results C[(i % 4) + 8 (i / 4) + 4 (l / 32)][l % 32], i = 0..15.  So a block of results whose columns stay (queries,
+// say) is the B operand of the next product as it lies in the registers, if that product takes its 16 summands in the order
+//   slot (l / 32, j)  <->  row 4 (l / 32) + j % 4 + 8 (j / 4)
+// and its A operand is read in the same order: two transposing LDS reads of four rows each (frag_t).  No value crosses lanes.
+#pragma once
+#include "common.h"
+
+namespace f3m {
+
+// one tensor of rows x heads x head_dim, strides in values
+struct Rows {
+    char *p;
+    int64_t row, head;
+};
+
+struct AttendArgs {
+    int batch, heads, kv_heads, group, dim;   // group = heads / kv_heads
+    int causal, window, sinks;
+    float scale;
+    int64_t total_q, total_k;
+    int max_q;
+    const int *q_offsets, *k_offsets;         // null: one sequence
+    Rows q, k, v, out;
+    float *lse;                               // (rows of q, heads)
+    // keys in pages (attention over a cache): pages of page_size rows, all heads of a page behind one another
+    const int *table, *lengths;               // table null: rows of k and v
+    int64_t table_row, pages;
+    int table_cols, page_shift;
+    const uint8_t *k_exp, *v_exp;             // 8-bit codes: exponent bytes of the rows
+    // the launch
+    int tiles, groups, pinned, chunk;         // row tiles of the longest sequence, batch * kv_heads, see block_of, key tiles of a part
+    int parts;                                // parts of the key axis; above 1 the results go to part_out, part_lse
+    float *part_out, *part_lse;               // (parts, rows of q, heads, dim) and (parts, rows of q, heads)
+    // gradient
+    Rows dout, dq, dk, dv;
+    float2 *stat;                             // (rows of q, heads): log2 of the row's sum (inf: empty row), dO.O
+};
+
+using s16x4 = __attribute__((ext_vector_type(4))) short;
+using s16x8 = __attribute__((ext_vector_type(8))) short;
+using f32x16 = __attribute__((ext_vector_type(16))) float;
+using f32x2 = __attribute__((ext_vector_type(2))) float;
+using u32x4 = __attribute__((ext_vector_type(4))) uint32_t;
+using u32x2 = __attribute__((ext_vector_type(2))) uint32_t;
+using bf16x8 = __attribute__((ext_vector_type(8))) __bf16;
+using bf16x2 = __attribute__((ext_vector_type(2))) __bf16;
+using f16x8 = __attribute__((ext_vector_type(8))) _Float16;
+using f16x2 = __attribute__((ext_vector_type(2))) _Float16;
+
+constexpr float LOG2E = 1.4426950408889634f, LN2 = 0.6931471805599453f;
+constexpr float NO_KEY = -__builtin_inff();
+
+struct Bf16 {
+    static constexpr bool narrow = false;          // fp32's range of exponents: no value needs scaling
+    static constexpr int nonfinite = 0x7f80;
+    static __device__ f32x16 mma(s16x8 a, s16x8 b, f32x16 c) {
+        return __builtin_amdgcn_mfma_f32_32x32x16_bf16(__builtin_bit_cast(bf16x8, a), __builtin_bit_cast(bf16x8, b), c, 0, 0, 0);
+    }
+    static __device__ uint32_t pack(float x, float y) {
+        return __builtin_bit_cast(uint32_t, __builtin_convertvector((f32x2){x, y}, bf16x2));
+    }
+    static __device__ float up(uint16_t x) { return __builtin_bit_cast(float, (uint32_t)x << 16); }
+    // two of the four e4m3 codes of w, times scale (a power of two): exact
+    template <bool HIGH> static __device__ uint32_t codes(uint32_t w, float scale) {
+        return __builtin_bit_cast(uint32_t, __builtin_amdgcn_cvt_scalef32_pk_bf16_fp8(w, scale, HIGH));
+    }
+};
+
+struct F16 {
+    static constexpr bool narrow = true;
+    static constexpr int nonfinite = 0x7c00;
+    static __device__ f32x16 mma(s16x8 a, s16x8 b, f32x16 c) {
+        return __builtin_amdgcn_mfma_f32_32x32x16_f16(__builtin_bit_cast(f16x8, a), __builtin_bit_cast(f16x8, b), c, 0, 0, 0);
+    }
+    static __device__ uint32_t pack(float x, float y) {
+        return __builtin_bit_cast(uint32_t, __builtin_convertvector((f32x2){x, y}, f16x2));
+    }
+    static __device__ float up(uint16_t x) { return (float)__builtin_bit_cast(_Float16, x); }
+    template <bool HIGH> static __device__ uint32_t codes(uint32_t w, float scale) {
+        return __builtin_bit_cast(uint32_t, __builtin_amdgcn_cvt_scalef32_pk_f16_fp8(w, scale, HIGH));
+    }
+};
+
+// attend.hip, attend_grad.hip: the launches, and the bytes of workspace that they need
+int64_t attend_workspace(AttendArgs a, int64_t max_k);
+void run_attend(AttendArgs a, int64_t max_k, bool f16, bool e8, void *workspace, hipStream_t st);
+int64_t attend_blocks(AttendArgs &a, int64_t items);
+int64_t attend_grad_workspace(const AttendArgs &a);
+void run_attend_grad(AttendArgs a, int64_t max_k, bool f16, void *workspace, hipStream_t st);
+// cache.hip
+void run_cache_rows(const f3m_cache &c, bool f16, const int64_t *slot, int64_t tokens, const f3m_rows &k, const f3m_rows &v, bool write,
+                    hipStream_t st);
+
+// ---- tiles in LDS: rows of DP values, their 16-byte pieces exchanged so that neither 8 rows read at one piece (frag_r) nor
+// 4 rows read at two neighbouring ones (frag_t) meet in a bank ----
+template <int DP> __device__ __forceinline__ int piece_swap(int r) {
+    if (DP == 128) return ((r & 7) << 1) ^ ((r >> 3) & 1);
+    if (DP == 64) return (r & 6) ^ ((r >> 3) & 1);
+    return (r >> 2) & 3;   // 32
+}
+template <int DP> __device__ __forceinline__ int tile_at(int r, int piece) {   // in values
+    return r * DP + ((piece ^ piece_swap<DP>(r)) << 3);
+}
+// A operand whose rows are rows of the tile: rows base .. base + 31, dimensions 16 ks .. 16 ks + 15
+template <int DP> __device__ __forceinline__ s16x8 frag_r(const short *tile, int base, int ks, int lane) {
+    return *(const s16x8 *)(tile + tile_at<DP>(base + (lane & 31), 2 * ks + (lane >> 5)));
+}
+using lds_s16x4 = __attribute__((address_space(3))) s16x4;
+// A operand whose rows are dimensions 32 db .. 32 db + 31 and whose summands are the tile's rows base .. base + 15, in the order above
+template <int DP> __device__ __forceinline__ s16x8 frag_t(const short *tile, int base, int db, int lane) {
+    const int i = lane & 15, r = base + 4 * (lane >> 5) + (i >> 2), piece = 4 * db + 2 * ((lane >> 4) & 1) + ((i & 3) >> 1), in = (i & 1) << 2;
+    s16x4 x = __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds_s16x4 *)(tile + tile_at<DP>(r, piece) + in));
+    s16x4 y = __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds_s16x4 *)(tile + tile_at<DP>(r + 8, piece) + in));
+    return __builtin_shufflevector(x, y, 0, 1, 2, 3, 4, 5, 6, 7);
+}
+
+// row of result i of a lane
+__device__ __forceinline__ int c_row(int i, int lane) { return (i & 3) + 8 * (i >> 2) + 4 * (lane >> 5); }
+
+__device__ __forceinline__ float both_halves_max(float x) {
+    auto r = __builtin_amdgcn_permlane32_swap(__builtin_bit_cast(uint32_t, x), __builtin_bit_cast(uint32_t, x), false, false);
+    return fmaxf(__builtin_bit_cast(float, (uint32_t)r[0]), __builtin_bit_cast(float, (uint32_t)r[1]));
+}
+__device__ __forceinline__ float both_halves_sum(float x) {
+    auto r = __builtin_amdgcn_permlane32_swap(__builtin_bit_cast(uint32_t, x), __builtin_bit_cast(uint32_t, x), false, false);
+    return __builtin_bit_cast(float, (uint32_t)r[0]) + __builtin_bit_cast(float, (uint32_t)r[1]);
+}
+
+// results 8 s .. 8 s + 7 of a block as a B operand
+template <class T> __device__ __forceinline__ s16x8 as_operand(const f32x16 &c, int s) {
+    u32x4 w;
+#pragma unroll
+    for (int j = 0; j < 4; ++j) w[j] = T::pack(c[8 * s + 2 * j], c[8 * s + 2 * j + 1]);
+    return __builtin_bit_cast(s16x8, w);
+}
+
+// Infinities and NaN in a row that is hidden from some columns must not reach those (0 * NaN = NaN in the product): where the mask
+// cuts a tile, operands are cleaned of them, and what they do to the columns that see them is put right otherwise.
+template <class T> __device__ __forceinline__ bool any_odd(u32x4 w) {
+    bool odd = false;
+#pragma unroll
+    for (int j = 0; j < 4; ++j)
+        odd |= (w[j] & (uint32_t)T::nonfinite) == (uint32_t)T::nonfinite || (w[j] >> 16 & (uint32_t)T::nonfinite) == (uint32_t)T::nonfinite;
+    return odd;
+}
+template <class T> __device__ __forceinline__ u32x4 cleaned(u32x4 w) {
+#pragma unroll
+    for (int j = 0; j < 4; ++j) {
+        if ((w[j] & (uint32_t)T::nonfinite) == (uint32_t)T::nonfinite) w[j] &= 0xffff0000u;
+        if ((w[j] >> 16 & (uint32_t)T::nonfinite) == (uint32_t)T::nonfinite) w[j] &= 0xffffu;
+    }
+    return w;
+}
+
+// ---- sequences ----
+struct Sequence {
+    int q0, nq, k0, nk;
+};
+// offsets outside the tensors, or that fall, give shorter or empty sequences and never an access out of range
+__device__ __forceinline__ Sequence sequence_of(const AttendArgs &a, int b) {
+    Sequence s;
+    int64_t q0 = 0, q1 = a.total_q, k0 = 0, k1 = a.total_k;
+    if (a.q_offsets) {
+        q0 = min(max((int64_t)a.q_offsets[b], (int64_t)0), a.total_q);
+        q1 = min(max((int64_t)a.q_offsets[b + 1], q0), a.total_q);
+    }
+    if (a.table) {
+        k0 = 0;
+        k1 = min(max((int64_t)a.lengths[b], (int64_t)0), (int64_t)a.table_cols << a.page_shift);
+    } else if (a.k_offsets) {
+        k0 = min(max((int64_t)a.k_offsets[b], (int64_t)0), a.total_k);
+        k1 = min(max((int64_t)a.k_offsets[b + 1], k0), a.total_k);
+    }
+    s.q0 = (int)q0; s.nq = (int)(q1 - q0); s.k0 = (int)k0; s.nk = (int)(k1 - k0);
+    return s;
+}
+
+// keys [lo, hi) and the first `sinks` below hi are visible to a token of the sequence
+struct Limits {
+    int lo, hi;
+};
+__device__ __forceinline__ Limits limits_of(const AttendArgs &a, const Sequence &s, int token) {
+    if (!a.causal) return {0, s.nk};
+    const int pos = s.nk - s.nq + token;
+    return {a.window && pos >= a.window ? pos - a.window + 1 : 0, pos + 1};
+}
+__device__ __forceinline__ bool sees(const Limits &m, int sinks, int key) { return key < m.hi && (key >= m.lo || key < sinks); }
+
+// key tiles of N rows that rows with limits from `first` to `last` see: the tiles of the sinks, then those of the window
+struct Tiles {
+    int sink, main0, count;   // tile n is n below sink, else main0 + n - sink
+    __device__ int operator[](int n) const { return n < sink ? n : main0 + n - sink; }
+};
+template <int N> __device__ __forceinline__ Tiles tiles_of(const Limits &first, const Limits &last, int sinks) {
+    const int end = last.hi > 0 ? (last.hi + N - 1) / N : 0, from = min(first.lo / N, end);
+    Tiles t;
+    t.sink = min(from, (sinks + N - 1) / N);
+    t.main0 = from;
+    t.count = t.sink + end - from;
+    return t;
+}
+
+// Work item of a block.  Blocks go round the 8 XCDs in turn, each with its own L2.  Pinned: all blocks of a group (sequence and key
+// head, which read the same keys) are on one XCD; without, groups are too few or would leave XCDs idle.  In both, the row tiles
+// come last to first over all groups: with causal order the long ones start first.
+struct Item {
+    int group, tile, part;
+};
+__device__ __forceinline__ Item block_of(const AttendArgs &a, uint32_t at) {
+    Item w;
+    uint32_t rest;
+    if (a.pinned) {
+        const uint32_t g8 = (uint32_t)(a.groups + 7) >> 3, j = at >> 3;
+        w.group = (int)((j % g8) * 8 + (at & 7));
+        rest = j / g8;
+    } else {
+        w.group = (int)(at % (uint32_t)a.groups);
+        rest = at / (uint32_t)a.groups;
+    }
+    w.tile = a.tiles - 1 - (int)(rest % (uint32_t)a.tiles);
+    w.part = (int)(rest / (uint32_t)a.tiles);
+    return w;
+}
+
+// ---- where the rows of K and V lie ----
+// Offset in values of row j of the sequence for key head hk, or in exponent bytes.  A page outside the cache is not touched: `ok`
+// comes back false and the offset is that of page 0.
+struct Place {
+    int64_t at, exp_at;
+    bool ok;
+};
+__device__ __forceinline__ Place place_of(const AttendArgs &a, const Sequence &s, int b, int hk, int j, const Rows &x) {
+    Place p;
+    if (!a.table) {
+        p.at = (int64_t)(s.k0 + j) * x.row + (int64_t)hk * x.head;
+        p.exp_at = 0;
+        p.ok = true;
+        return p;
+    }
+    const int page = a.table[(int64_t)b * a.table_row + (j >> a.page_shift)];
+    p.ok = page >= 0 && page < a.pages;
+    p.exp_at = (((int64_t)(p.ok ? page : 0) * a.kv_heads + hk) << a.page_shift) + (j & ((1 << a.page_shift) - 1));
+    p.at = p.exp_at * a.dim;
+    return p;
+}
+
+// 16 bytes of zeros where the tile is wider than the head
+template <int DP> __device__ __forceinline__ u32x4 load_piece(const char *base, int64_t at, int piece, int dim) {
+    if (piece * 8 >= dim) return (u32x4){0, 0, 0, 0};
+    return *(const u32x4 *)(base + 2 * (at + piece * 8));
+}
+
+// a row of results (C layout, columns are rows of the tensor) to 16-bit values: halves exchange four values so that each lane
+// stores 16 bytes; `scale` is the lane's
+template <class T, int DB>
+__device__ __forceinline__ void store_rows(const f32x16 (&acc)[DB], float scale, char *base, int64_t at, int dim, bool valid, int lane) {
+#pragma unroll
+    for (int db = 0; db < DB; ++db)
+#pragma unroll
+        for (int s = 0; s < 2; ++s) {
+            uint32_t w[4];
+#pragma unroll
+            for (int j = 0; j < 4; ++j) w[j] = T::pack(acc[db][8 * s + 2 * j] * scale, acc[db][8 * s + 2 * j + 1] * scale);
+            auto x = __builtin_amdgcn_permlane32_swap(w[0], w[2], false, false);
+            auto y = __builtin_amdgcn_permlane32_swap(w[1], w[3], false, false);
+            const int d = 32 * db + 16 * s + 8 * (lane >> 5);
+            if (valid && d < dim) *(u32x4 *)(base + 2 * (at + d)) = (u32x4){(uint32_t)x[0], (uint32_t)y[0], (uint32_t)x[1], (uint32_t)y[1]};
+        }
+}
+
+}  // namespace f3m

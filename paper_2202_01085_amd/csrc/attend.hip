@@ -1,0 +1,455 @@
+// Row-normalised products (attention), forward: o_i = sum_j w_ij v_j, w_ij = exp(scale q_i.k_j) / (its sum over the visible j).
+//
+// Rows of a work item are (token, query head) pairs that share a key head, 32 to a wave.  A wave keeps its rows' q and o in
+// registers and goes over the keys once, with the running maximum m and sum l of each row (one row to a lane pair): a block of
+// scores S^T = K Q^T, weights exp2(c s - c m), o^T = o^T exp2(c m_old - c m) + V^T w^T.  m moves only when a score is above it by
+// 2^8 or more, so o is rarely rescaled; weights stay below 2^8 and their sums in fp32 (fp16 weights are held times 2^7, so that
+// they keep 11 bits down to 2^-21 of the largest).  The weights are rounded to the inputs' type for the matrix cores.
+#include "attend.h"
+
+#include <algorithm>
+
+namespace f3m {
+
+namespace {
+
+constexpr int NT = 256;       // four waves
+constexpr int KT = 64;        // keys of a tile
+constexpr float GROW = 8.f;   // log2 of how far a score may lie above m
+
+// Pieces of a tile of K and V on their way from memory to LDS, N rows for THREADS threads
+template <class T, int DP, bool E8, int N, int THREADS> struct Stage {
+    static constexpr int VALUES = E8 ? 16 : 8, PIECES = DP / VALUES, COUNT = (N * PIECES + THREADS - 1) / THREADS;
+    static constexpr bool ALL = N * PIECES % THREADS == 0;
+    u32x4 k[COUNT], v[COUNT];
+    uint8_t ke[COUNT], ve[COUNT];
+
+    __device__ void load(const AttendArgs &a, const Sequence &s, int b, int hk, int key0, int tid) {
+#pragma unroll
+        for (int c = 0; c < COUNT; ++c) {
+            const int at = tid + THREADS * c, row = at / PIECES, piece = at % PIECES;
+            if (!ALL && row >= N) break;
+            const int j = min(key0 + row, s.nk - 1);
+            const Place p = place_of(a, s, b, hk, j, a.k);
+            const int64_t vat = a.table ? p.at : (int64_t)(s.k0 + j) * a.v.row + (int64_t)hk * a.v.head;
+            if (E8) {
+                const bool in = piece * 16 < a.dim;
+                k[c] = in ? *(const u32x4 *)(a.k.p + p.at + piece * 16) : (u32x4){0, 0, 0, 0};
+                v[c] = in ? *(const u32x4 *)(a.v.p + p.at + piece * 16) : (u32x4){0, 0, 0, 0};
+                ke[c] = a.k_exp[p.exp_at];
+                ve[c] = a.v_exp[p.exp_at];
+            } else {
+                k[c] = load_piece<DP>(a.k.p, p.at, piece, a.dim);
+                v[c] = load_piece<DP>(a.v.p, vat, piece, a.dim);
+            }
+        }
+    }
+    static __device__ bool put(short *tile, int row, int piece, u32x4 x, uint8_t e, bool clean) {
+        bool odd = false;
+        if (E8) {
+            const float scale = __builtin_bit_cast(float, (uint32_t)e << 23);
+#pragma unroll
+            for (int h = 0; h < 2; ++h) {
+                u32x4 w = {T::template codes<false>(x[2 * h], scale), T::template codes<true>(x[2 * h], scale),
+                           T::template codes<false>(x[2 * h + 1], scale), T::template codes<true>(x[2 * h + 1], scale)};
+                if (clean && any_odd<T>(w)) {
+                    w = cleaned<T>(w);
+                    odd = true;
+                }
+                *(u32x4 *)(tile + tile_at<DP>(row, 2 * piece + h)) = w;
+            }
+        } else {
+            if (clean && any_odd<T>(x)) {
+                x = cleaned<T>(x);
+                odd = true;
+            }
+            *(u32x4 *)(tile + tile_at<DP>(row, piece)) = x;
+        }
+        return odd;
+    }
+    // to LDS; with `clean`, infinities and NaN of v become 0 and the rows that had one come back as bits (a wave's)
+    __device__ uint64_t store(short *kt, short *vt, int tid, bool clean) const {
+        uint64_t odd = 0;
+#pragma unroll
+        for (int c = 0; c < COUNT; ++c) {
+            const int at = tid + THREADS * c, row = at / PIECES, piece = at % PIECES;
+            if (!ALL && row >= N) break;
+            put(kt, row, piece, k[c], ke[c], false);
+            if (put(vt, row, piece, v[c], ve[c], clean)) odd |= 1ull << row;
+        }
+        if (!clean || !__any(odd != 0)) return 0;
+#pragma unroll 1
+        for (int by = 32; by > 0; by >>= 1) odd |= __shfl_xor((unsigned long long)odd, by);
+        return odd;
+    }
+};
+
+// which rows of a tile lie in pages of the cache (bit r: row key0 + r), for lanes r of one wave
+__device__ __forceinline__ uint64_t good_pages(const AttendArgs &a, const Sequence &s, int b, int key0, int lane) {
+    if (!a.table) return ~0ull;
+    const int j = min(key0 + lane, s.nk - 1);
+    const int page = a.table[(int64_t)b * a.table_row + (j >> a.page_shift)];
+    return __ballot(page >= 0 && page < a.pages);
+}
+
+// what a wave carries from tile to tile
+template <class T, int DP> struct Rows32 {
+    static constexpr int KS = DP / 16, DB = DP / 32;
+    static constexpr float LIFT = T::narrow ? 7.f : 0.f;   // log2 of the factor that weights are held with
+    s16x8 q[KS];
+    f32x16 o[DB];
+    float m, l;        // largest score so far as used, sum of the weights (of this lane's half of the keys) times 2^LIFT
+    float spoil;       // 0, or NaN once the row (in this lane's half) has seen an odd v
+
+    __device__ void start(const AttendArgs &a, const char *base, int64_t at, int lane) {
+#pragma unroll
+        for (int ks = 0; ks < KS; ++ks) q[ks] = __builtin_bit_cast(s16x8, load_piece<DP>(base, at, 2 * ks + (lane >> 5), a.dim));
+#pragma unroll
+        for (int db = 0; db < DB; ++db) o[db] = (f32x16)0.f;
+        m = NO_KEY;
+        l = 0.f;
+        spoil = 0.f;
+    }
+
+    // NB blocks of 32 keys from key0 on, whose rows lie in LDS from row 0 on.  edge: the mask cuts the tile for some row, or `good` (rows
+    // in pages of the cache) or `odd` (rows whose infinities or NaN in v are cleaned away) say something
+    template <int NB>
+    __device__ void step(const short *kt, const short *vt, int key0, bool edge, uint64_t good, uint64_t odd, const Limits &mine, int sinks, float c, int lane) {
+        f32x16 s[NB];
+#pragma unroll
+        for (int kb = 0; kb < NB; ++kb) {
+            s[kb] = (f32x16)0.f;
+#pragma unroll
+            for (int ks = 0; ks < KS; ++ks) s[kb] = T::mma(frag_r<DP>(kt, 32 * kb, ks, lane), q[ks], s[kb]);
+        }
+        if (edge) {
+            bool spoilt = false;
+#pragma unroll
+            for (int kb = 0; kb < NB; ++kb)
+#pragma unroll
+                for (int i = 0; i < 16; ++i) {
+                    const int r = 32 * kb + c_row(i, lane);
+                    const bool seen = sees(mine, sinks, key0 + r) && ((good >> r) & 1);
+                    s[kb][i] = seen ? s[kb][i] : NO_KEY;
+                    spoilt |= seen && ((odd >> r) & 1);
+                }
+            spoil = spoilt ? __builtin_nanf("") : spoil;
+        }
+        float top = s[0][0];
+#pragma unroll
+        for (int kb = 0; kb < NB; ++kb)
+#pragma unroll
+            for (int i = 0; i < 16; ++i) top = fmaxf(top, s[kb][i]);
+        top = both_halves_max(top);
+        if (__any((top - m) * c > GROW)) {         // m = -inf: the difference is inf, or NaN while nothing is visible
+            const float now = fmaxf(m, top), by = m == now ? 1.f : __builtin_amdgcn_exp2f((m - now) * c);
+            m = now;
+            l *= by;
+#pragma unroll
+            for (int db = 0; db < DB; ++db)
+#pragma unroll
+                for (int i = 0; i < 16; ++i) o[db][i] *= by;
+        }
+        const float base = m == NO_KEY ? 0.f : LIFT - m * c;
+#pragma unroll
+        for (int kb = 0; kb < NB; ++kb) {
+            float sum = 0.f;
+#pragma unroll
+            for (int i = 0; i < 16; ++i) {
+                s[kb][i] = __builtin_amdgcn_exp2f(__builtin_fmaf(s[kb][i], c, base));
+                sum += s[kb][i];
+            }
+            l += sum;
+#pragma unroll
+            for (int h = 0; h < 2; ++h) {
+                const s16x8 w = as_operand<T>(s[kb], h);
+#pragma unroll
+                for (int db = 0; db < DB; ++db) o[db] = T::mma(frag_t<DP>(vt, 32 * kb + 16 * h, db, lane), w, o[db]);
+            }
+        }
+    }
+    // the logarithm of the row's sum, in natural units
+    __device__ float lse(float all, float c) const { return all > 0.f ? (m * c - LIFT + __builtin_amdgcn_logf(all)) * LN2 : all == all ? NO_KEY : all; }
+};
+
+// Many rows: a work item is 128 rows of one group, the four waves share tiles of 64 keys.  Bound by the matrix cores and by
+// what LDS delivers to them (one operand of each product comes from there).
+template <class T, int DP, bool E8> __global__ __launch_bounds__(NT, 2) void attend_many(AttendArgs a) {
+    using Row = Rows32<T, DP>;
+    __shared__ __attribute__((aligned(16))) short tile[2][2][KT * DP];
+    __shared__ uint64_t good_rows[2], odd_rows[2][4];
+    const Item it = block_of(a, blockIdx.x);
+    if (it.group >= a.groups) return;
+    const int b = it.group / a.kv_heads, hk = it.group % a.kv_heads;
+    const Sequence s = sequence_of(a, b);
+    const int rows = min(s.nq, a.max_q) * a.group, r0 = it.tile * 128;
+    if (r0 >= rows) return;
+    const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6);
+
+    const Limits first = limits_of(a, s, r0 / a.group), last = limits_of(a, s, min(r0 + 127, rows - 1) / a.group);
+    const Tiles tiles = tiles_of<KT>(first, last, a.sinks);
+    int n = it.part * a.chunk, end = tiles.count;
+    if (a.parts > 1) end = min(end, n + a.chunk);
+
+    const int w0 = r0 + 32 * wave, row = min(w0 + (lane & 31), rows - 1), token = row / a.group, head = hk * a.group + row % a.group;
+    const bool valid = w0 + (lane & 31) < rows;
+    const Limits mine = limits_of(a, s, token);
+    const Limits wfirst = limits_of(a, s, min(w0, rows - 1) / a.group), wlast = limits_of(a, s, min(w0 + 31, rows - 1) / a.group);
+    const bool idle = w0 >= rows;
+    const float c = a.scale * LOG2E;
+
+    Row r;
+    r.start(a, a.q.p, (int64_t)(s.q0 + token) * a.q.row + (int64_t)head * a.q.head, lane);
+    if (n < end) {
+        Stage<T, DP, E8, KT, NT> next;
+        uint64_t good = 0;
+        auto fetch = [&](int t) {
+            next.load(a, s, b, hk, tiles[t] * KT, tid);
+            if (wave == 0) good = good_pages(a, s, b, tiles[t] * KT, lane);
+        };
+        auto keep = [&](int t, int buf) {
+            const int key0 = tiles[t] * KT;
+            const uint64_t odd = next.store(tile[buf][0], tile[buf][1], tid, !(key0 + KT <= first.hi && (key0 >= last.lo || key0 + KT <= a.sinks)));
+            if (lane == 0) odd_rows[buf][wave] = odd;
+            if (tid == 0) good_rows[buf] = good;
+        };
+        fetch(n);
+        keep(n, n & 1);
+        __syncthreads();
+        for (; n < end; ++n) {
+            const int buf = n & 1, key0 = tiles[n] * KT;
+            if (n + 1 < end) fetch(n + 1);
+            const uint64_t ok = good_rows[buf], odd = odd_rows[buf][0] | odd_rows[buf][1] | odd_rows[buf][2] | odd_rows[buf][3];
+            const bool none = idle || key0 >= wlast.hi || (key0 + KT <= wfirst.lo && key0 >= a.sinks);
+            const bool full = key0 + KT <= wfirst.hi && (key0 >= wlast.lo || key0 + KT <= a.sinks) && ok == ~0ull && odd == 0;
+            if (!none) r.template step<2>(tile[buf][0], tile[buf][1], key0, !full, ok, odd, mine, a.sinks, c, lane);
+            if (n + 1 < end) keep(n + 1, buf ^ 1);
+            __syncthreads();
+        }
+    }
+    const float all = both_halves_sum(r.l), by = both_halves_sum(r.spoil) + (all > 0.f ? 1.f / all : all == all ? 0.f : all);
+    const int64_t at_row = (int64_t)(s.q0 + token) * a.heads + head;
+    if (a.parts > 1) {
+        const int64_t at = (int64_t)it.part * a.total_q * a.heads + at_row;
+        if (valid) {
+            if (lane < 32) a.part_lse[at] = r.lse(all, c);
+#pragma unroll
+            for (int db = 0; db < Row::DB; ++db)
+#pragma unroll
+                for (int i = 0; i < 16; i += 4) {
+                    const int d = 32 * db + c_row(i, lane);
+                    if (d < a.dim) *(float4 *)(a.part_out + at * a.dim + d) = make_float4(r.o[db][i] * by, r.o[db][i + 1] * by, r.o[db][i + 2] * by, r.o[db][i + 3] * by);
+                }
+        }
+        return;
+    }
+    if (valid && lane < 32) a.lse[at_row] = r.lse(all, c);
+    store_rows<T, Row::DB>(r.o, by, a.out.p, (int64_t)(s.q0 + token) * a.out.row + (int64_t)head * a.out.head, a.dim, valid, lane);
+}
+
+// Few rows (single tokens, short chunks): a work item is 32 rows and a part of the keys; each of the four waves takes every fourth
+// tile of 32 keys through LDS of its own, and the four results are joined at the end.  Bound by the reading of K and V.
+template <class T, int DP, bool E8> __global__ __launch_bounds__(NT, 2) void attend_few(AttendArgs a) {
+    using Row = Rows32<T, DP>;
+    constexpr int N = 32;
+    __shared__ __attribute__((aligned(16))) short tile[4][2][N * DP];
+    __shared__ float joined[4][2][32];
+    const Item it = block_of(a, blockIdx.x);
+    if (it.group >= a.groups) return;
+    const int b = it.group / a.kv_heads, hk = it.group % a.kv_heads;
+    const Sequence s = sequence_of(a, b);
+    const int rows = min(s.nq, a.max_q) * a.group, r0 = it.tile * 32;
+    if (r0 >= rows) return;
+    const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6);
+    const Limits first = limits_of(a, s, r0 / a.group), last = limits_of(a, s, min(r0 + 31, rows - 1) / a.group);
+    const Tiles tiles = tiles_of<N>(first, last, a.sinks);
+    int n = it.part * a.chunk + wave, end = tiles.count;
+    if (a.parts > 1) end = min(end, (it.part + 1) * a.chunk);
+    const int row = min(r0 + (lane & 31), rows - 1), token = row / a.group, head = hk * a.group + row % a.group;
+    const bool valid = r0 + (lane & 31) < rows;
+    const int64_t at_row = (int64_t)(s.q0 + token) * a.heads + head;
+    if (it.part * a.chunk >= tiles.count && it.part > 0) {   // nothing here: the part counts as empty
+        if (wave == 0 && lane < 32 && valid) a.part_lse[(int64_t)it.part * a.total_q * a.heads + at_row] = NO_KEY;
+        return;
+    }
+    const Limits mine = limits_of(a, s, token);
+    const float c = a.scale * LOG2E;
+
+    Row r;
+    r.start(a, a.q.p, (int64_t)(s.q0 + token) * a.q.row + (int64_t)head * a.q.head, lane);
+    short *kt = tile[wave][0], *vt = tile[wave][1];
+    if (n < end) {
+        Stage<T, DP, E8, N, 64> next;
+        next.load(a, s, b, hk, tiles[n] * N, lane);
+        uint64_t good = good_pages(a, s, b, tiles[n] * N, lane);
+        for (; n < end; n += 4) {
+            const int key0 = tiles[n] * N;
+            const bool whole = key0 + N <= first.hi && (key0 >= last.lo || key0 + N <= a.sinks) && (uint32_t)good == ~0u;
+            const uint64_t odd = next.store(kt, vt, lane, !whole);
+            const uint64_t ok = good;
+            if (n + 4 < end) {
+                next.load(a, s, b, hk, tiles[n + 4] * N, lane);
+                good = good_pages(a, s, b, tiles[n + 4] * N, lane);
+            }
+            __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");   // LDS does a wave's accesses in their order: nothing to wait for
+            r.template step<1>(kt, vt, key0, !whole, ok, odd, mine, a.sinks, c, lane);
+            __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");
+        }
+    }
+    // join: every wave's o in the common unit, summed over the waves from LDS
+    const float all = both_halves_sum(r.l);
+    if (lane < 32) { joined[wave][0][lane] = r.m; joined[wave][1][lane] = all; }
+    __syncthreads();
+    float top = NO_KEY, sum = 0.f;
+#pragma unroll
+    for (int w = 0; w < 4; ++w) top = fmaxf(top, joined[w][0][lane & 31]);
+#pragma unroll
+    for (int w = 0; w < 4; ++w) {
+        const float m = joined[w][0][lane & 31];
+        sum += m == NO_KEY && joined[w][1][lane & 31] == 0.f ? 0.f : joined[w][1][lane & 31] * __builtin_amdgcn_exp2f((m - top) * c);
+    }
+    const float spoil = both_halves_sum(r.spoil);
+    const float unit = all == 0.f ? 0.f : __builtin_amdgcn_exp2f((r.m - top) * c), by = spoil + (sum > 0.f ? unit / sum : sum == sum ? 0.f : sum);
+    r.m = top;
+    float *mine_o = (float *)tile[wave];       // 32 x DP values, the two tiles' 4 * 32 * DP bytes
+#pragma unroll
+    for (int db = 0; db < Row::DB; ++db)
+#pragma unroll
+        for (int i = 0; i < 16; i += 4) {
+            const int d4 = (32 * db + c_row(i, lane)) >> 2;
+            *(float4 *)(mine_o + (lane & 31) * DP + (((d4 ^ (lane & 7)) << 2))) = make_float4(r.o[db][i] * by, r.o[db][i + 1] * by, r.o[db][i + 2] * by, r.o[db][i + 3] * by);
+        }
+    if (wave == 0 && lane < 32 && valid) {
+        const float y = r.lse(sum, c);
+        if (a.parts > 1) a.part_lse[(int64_t)it.part * a.total_q * a.heads + at_row] = y;
+        else a.lse[at_row] = y;
+    }
+    __syncthreads();
+    for (int at = tid; at < 32 * (DP / 8); at += NT) {
+        const int x = at / (DP / 8), d = at % (DP / 8) * 8;
+        if (r0 + x >= rows || d >= a.dim) continue;
+        float y[8];
+#pragma unroll
+        for (int h = 0; h < 2; ++h) {
+            float4 t = make_float4(0.f, 0.f, 0.f, 0.f);
+#pragma unroll
+            for (int w = 0; w < 4; ++w) {
+                const float4 u = *(const float4 *)((const float *)tile[w] + x * DP + ((((d >> 2) + h) ^ (x & 7)) << 2));
+                t.x += u.x; t.y += u.y; t.z += u.z; t.w += u.w;
+            }
+            y[4 * h] = t.x; y[4 * h + 1] = t.y; y[4 * h + 2] = t.z; y[4 * h + 3] = t.w;
+        }
+        const int tk = (r0 + x) / a.group, hd = hk * a.group + (r0 + x) % a.group;
+        if (a.parts > 1) {
+            float *to = a.part_out + (((int64_t)it.part * a.total_q + s.q0 + tk) * a.heads + hd) * a.dim + d;
+            *(float4 *)to = make_float4(y[0], y[1], y[2], y[3]);
+            *(float4 *)(to + 4) = make_float4(y[4], y[5], y[6], y[7]);
+        } else {
+            *(u32x4 *)(a.out.p + 2 * ((int64_t)(s.q0 + tk) * a.out.row + (int64_t)hd * a.out.head + d)) =
+                (u32x4){T::pack(y[0], y[1]), T::pack(y[2], y[3]), T::pack(y[4], y[5]), T::pack(y[6], y[7])};
+        }
+    }
+}
+
+// The parts of each row joined: 32 lanes to a row, four dimensions each.  Rows of no sequence have no parts and are left alone.
+template <class T> __global__ __launch_bounds__(NT) void join_parts(AttendArgs a) {
+    const int64_t row = (int64_t)blockIdx.x * 8 + threadIdx.x / 32, all = a.total_q * a.heads;
+    if (row >= all) return;
+    const int x = threadIdx.x % 32 * 4;
+    const int64_t token = row / a.heads;
+    const int head = (int)(row % a.heads);
+    if (a.q_offsets) {
+        // the sequence of the token: the last offset not above it
+        int lo = 0, hi = a.batch;
+        while (lo < hi) {
+            const int mid = (lo + hi) / 2;
+            if (a.q_offsets[mid + 1] <= token) lo = mid + 1;
+            else hi = mid;
+        }
+        if (lo == a.batch || token < a.q_offsets[lo]) return;
+        if (token - a.q_offsets[lo] >= a.max_q) return;
+    } else if (token >= a.max_q) {
+        return;
+    }
+    float top = NO_KEY;
+    for (int p = 0; p < a.parts; ++p) top = fmaxf(top, a.part_lse[p * all + row]);
+    float sum = 0.f;
+    float4 o = make_float4(0.f, 0.f, 0.f, 0.f);
+    for (int p = 0; p < a.parts; ++p) {
+        const float l = a.part_lse[p * all + row];
+        if (l == NO_KEY) continue;
+        const float w = __builtin_amdgcn_exp2f((l - top) * LOG2E);
+        sum += w;
+        if (x < a.dim) {
+            const float4 u = *(const float4 *)(a.part_out + (p * all + row) * a.dim + x);
+            o.x += w * u.x; o.y += w * u.y; o.z += w * u.z; o.w += w * u.w;
+        }
+    }
+    const float by = sum > 0.f ? 1.f / sum : sum == sum ? 0.f : sum;
+    if (x == 0) a.lse[row] = sum > 0.f ? top + __builtin_amdgcn_logf(sum) * LN2 : sum == sum ? NO_KEY : sum;
+    if (x < a.dim)
+        *(u32x2 *)(a.out.p + 2 * (token * a.out.row + (int64_t)head * a.out.head + x)) = (u32x2){T::pack(o.x * by, o.y * by), T::pack(o.z * by, o.w * by)};
+}
+
+// key tiles of `per` rows that a work item of `rows` (token, head) rows may see at most
+int64_t most_tiles(const AttendArgs &a, int64_t max_k, int rows, int per) {
+    int64_t t = cdiv(max_k, per);
+    if (a.window) t = std::min(t, cdiv(rows, a.group) / per + a.window / per + 4 + cdiv(a.sinks, per));
+    return std::max<int64_t>(t, 1);
+}
+
+template <class T, int DP, bool E8> void launch(const AttendArgs &a, bool few, int64_t blocks, hipStream_t st) {
+    if (few) attend_few<T, DP, E8><<<dim3((uint32_t)blocks), NT, 0, st>>>(a);
+    else attend_many<T, DP, E8><<<dim3((uint32_t)blocks), NT, 0, st>>>(a);
+    F3M_HIP(hipGetLastError());
+    if (a.parts > 1) {
+        join_parts<T><<<dim3((uint32_t)cdiv(a.total_q * a.heads, 8)), NT, 0, st>>>(a);
+        F3M_HIP(hipGetLastError());
+    }
+}
+
+template <class T> void launch_dim(const AttendArgs &a, bool e8, bool few, int64_t blocks, hipStream_t st) {
+    if (a.dim <= 32) e8 ? launch<T, 32, true>(a, few, blocks, st) : launch<T, 32, false>(a, few, blocks, st);
+    else if (a.dim <= 64) e8 ? launch<T, 64, true>(a, few, blocks, st) : launch<T, 64, false>(a, few, blocks, st);
+    else e8 ? launch<T, 128, true>(a, few, blocks, st) : launch<T, 128, false>(a, few, blocks, st);
+}
+
+// Up to 64 rows to a key head go to attend_few.  A long key axis is cut into parts where the rows alone make too few blocks: two
+// blocks fit a CU, 512 the device.
+bool split(AttendArgs &a, int64_t max_k) {
+    const bool few = (int64_t)a.max_q * a.group <= 64;
+    const int per = few ? 32 : KT, rows = few ? 32 : 128, least = few ? 16 : 8;
+    a.tiles = (int)cdiv((int64_t)a.max_q * a.group, rows);
+    const int64_t most = most_tiles(a, max_k, rows, per), items = (int64_t)a.tiles * a.groups;
+    const int64_t want = few ? cdiv(2048, items) : items >= 512 ? 1 : cdiv(1024, items);
+    a.chunk = (int)std::max<int64_t>(cdiv(most, want), std::min<int64_t>(least, most));
+    a.parts = (int)cdiv(most, a.chunk);
+    return few;
+}
+
+}  // namespace
+
+int64_t attend_workspace(AttendArgs a, int64_t max_k) {
+    if (!a.max_q || !a.total_q || !a.groups) return 0;
+    split(a, max_k);
+    return a.parts > 1 ? (int64_t)a.parts * a.total_q * a.heads * (a.dim + 1) * (int64_t)sizeof(float) : 0;
+}
+
+void run_attend(AttendArgs a, int64_t max_k, bool f16, bool e8, void *workspace, hipStream_t st) {
+    if (!a.max_q || !a.total_q || !a.groups) return;
+    const bool few = split(a, max_k);
+    a.part_out = (float *)workspace;
+    a.part_lse = a.part_out ? a.part_out + (int64_t)a.parts * a.total_q * a.heads * a.dim : nullptr;
+    const int64_t blocks = attend_blocks(a, (int64_t)a.tiles * a.parts);
+    f16 ? launch_dim<F16>(a, e8, few, blocks, st) : launch_dim<Bf16>(a, e8, few, blocks, st);
+}
+
+// sets a.pinned; blocks of a launch with `items` to a group
+int64_t attend_blocks(AttendArgs &a, int64_t items) {
+    a.pinned = a.groups % 8 == 0 || a.groups >= 64;
+    const int64_t blocks = (a.pinned ? cdiv(a.groups, 8) * 8 : a.groups) * items;
+    if (blocks > (1 << 24) - 1) fail(F3M_ERR_UNSUPPORTED, "attention: too many work items for one call (2^24)");
+    return blocks;
+}
+
+}  // namespace f3m

@@ -65,6 +65,26 @@ class Times(ctypes.Structure):
         return {k: float(getattr(self, k)) for k, _ in self._fields_}
 
 
+class Rows(ctypes.Structure):
+    _fields_ = [("data", ctypes.c_void_p), ("row", ctypes.c_int64), ("head", ctypes.c_int64)]
+
+
+class AttentionArgs(ctypes.Structure):
+    _fields_ = [("dtype", ctypes.c_int32), ("batch", ctypes.c_int32), ("heads", ctypes.c_int32), ("kv_heads", ctypes.c_int32),
+                ("head_dim", ctypes.c_int32), ("causal", ctypes.c_int32), ("window", ctypes.c_int32), ("sinks", ctypes.c_int32),
+                ("scale", ctypes.c_float), ("max_q", ctypes.c_int32), ("max_k", ctypes.c_int32), ("total_q", ctypes.c_int64),
+                ("total_k", ctypes.c_int64), ("q_offsets", ctypes.c_void_p), ("k_offsets", ctypes.c_void_p),
+                ("q", Rows), ("k", Rows), ("v", Rows)]
+
+
+class CacheInfo(ctypes.Structure):
+    _fields_ = [("held", ctypes.c_int32), ("kv_heads", ctypes.c_int32), ("head_dim", ctypes.c_int32), ("page_size", ctypes.c_int32),
+                ("pages", ctypes.c_int64), ("k", ctypes.c_void_p), ("v", ctypes.c_void_p), ("k_exp", ctypes.c_void_p),
+                ("v_exp", ctypes.c_void_p)]
+
+
+DTYPES = {torch.bfloat16: 0, torch.float16: 1, torch.float8_e4m3fn: 2}
+
 _lib = None
 
 
@@ -107,6 +127,16 @@ def lib():
         L.f3m_plan_get_list.argtypes = [vp, ci, ci, vp, vp]
         L.f3m_stage_times.argtypes = [vp, ctypes.POINTER(Times)]
         L.f3m_level_times.argtypes = [vp, ci, vp]
+        args, rows, cache = ctypes.POINTER(AttentionArgs), ctypes.POINTER(Rows), ctypes.POINTER(CacheInfo)
+        L.f3m_attention_workspace.argtypes = [args]
+        L.f3m_attention_grad_workspace.argtypes = [args]
+        L.f3m_attention_workspace.restype = L.f3m_attention_grad_workspace.restype = i64
+        L.f3m_attention.argtypes = [args, rows, vp, vp, i64, vp]
+        L.f3m_attention_grad.argtypes = [args, rows, rows, vp, rows, rows, rows, vp, i64, vp]
+        L.f3m_cache_write.argtypes = L.f3m_cache_read.argtypes = [cache, ci, rows, rows, vp, i64, vp]
+        L.f3m_cache_attention.argtypes = [cache, args, vp, i64, ctypes.c_int32, vp, rows, vp, vp, i64, vp]
+        for name in ("f3m_attention", "f3m_attention_grad", "f3m_cache_write", "f3m_cache_read", "f3m_cache_attention"):
+            getattr(L, name).restype = ci
         for name in ("f3m_plan", "f3m_plan_ex", "f3m_kmvm", "direct_kmvm", "direct_kmvm_rows_f64", "f3m_plan_info",
                      "f3m_plan_get_perm", "f3m_plan_get_point_keys", "f3m_plan_get_boxes", "f3m_plan_get_list",
                      "f3m_stage_times", "f3m_level_times", "f3m_plan_xy", "direct_kmvm_xy", "direct_kmvm_xy_rows_f64",
@@ -349,3 +379,213 @@ def direct_kmvm_xy_rows_f64(X, Y, b, lengthscale, rows, stream=None):
                                          ctypes.c_void_p(rows.data_ptr()), int(rows.numel()),
                                          ctypes.c_void_p(y64.data_ptr()), _stream(stream)))
     return y64
+
+
+# ---- row-normalised products (attention) ----
+
+class _On:
+    """The device of the call's tensors made current, and the call's stream: what the binding allocates belongs to that stream."""
+
+    def __init__(self, device, stream):
+        self.stream = torch.cuda.current_stream(device) if stream is None else stream
+        if self.stream.device != device:
+            raise ValueError("the stream is of %s, the tensors are on %s" % (self.stream.device, device))
+        self._scope = torch.cuda.stream(self.stream)     # also makes the stream's device current
+        self.handle = ctypes.c_void_p(self.stream.cuda_stream)
+
+    def __enter__(self):
+        self._scope.__enter__()
+        return self
+
+    def __exit__(self, *e):
+        return self._scope.__exit__(*e)
+
+
+def _rows(t, name, like=None, heads=None, rows=None):
+    """a (rows, heads, head_dim) device tensor, head_dim contiguous, as the library takes it"""
+    if not (isinstance(t, torch.Tensor) and t.is_cuda and t.dim() == 3 and t.dtype in (torch.bfloat16, torch.float16)):
+        raise TypeError("%s must be a device tensor (rows, heads, head_dim) of bfloat16 or float16" % name)
+    if like is not None and (t.dtype != like.dtype or t.device != like.device or t.shape[2] != like.shape[2]):
+        raise ValueError("%s must have the type, the device and the head_dim of the other tensors" % name)
+    if heads is not None and t.shape[1] != heads or rows is not None and t.shape[0] != rows:
+        raise ValueError("%s must have shape (%s, %s, head_dim)" % (name, "rows" if rows is None else rows, "heads" if heads is None else heads))
+    if t.shape[2] > 1 and t.stride(2) != 1:
+        raise ValueError("%s must be contiguous along head_dim" % name)
+    row, head = t.stride(0) if t.shape[0] > 1 else t.shape[2], t.stride(1) if t.shape[1] > 1 else t.shape[2]
+    if t.numel() and (t.data_ptr() % 16 or row % 8 or head % 8):
+        raise ValueError("%s must be 16-byte aligned, with strides that are multiples of 8" % name)
+    return Rows(t.data_ptr() if t.numel() else None, row, head)
+
+
+def _device_array(t, name, dtype, device, shape):
+    if not (isinstance(t, torch.Tensor) and t.is_cuda and t.dtype == dtype and t.device == device):
+        raise TypeError("%s must be a %s tensor on %s" % (name, str(dtype).replace("torch.", ""), device))
+    if t.shape != shape or not t.is_contiguous():
+        raise ValueError("%s must be contiguous and have shape %s" % (name, tuple(shape)))
+    return t.data_ptr() if t.numel() else None
+
+
+def _lse(lse, rows, heads, device):
+    if lse is None:
+        return torch.empty((rows, heads), dtype=torch.float32, device=device)
+    _device_array(lse, "lse", torch.float32, device, (rows, heads))
+    return lse
+
+
+def _attention_args(q, kv_heads, q_offsets, max_q, scale, causal, window, sinks):
+    a = AttentionArgs()
+    a.q = _rows(q, "q")
+    a.dtype, a.heads, a.kv_heads, a.head_dim = DTYPES[q.dtype], q.shape[1], kv_heads, q.shape[2]
+    a.causal, a.window, a.sinks = int(bool(causal)), int(window), int(sinks)
+    a.scale = 1.0 / q.shape[2] ** 0.5 if scale is None and q.shape[2] else float(1.0 if scale is None else scale)
+    a.total_q = q.shape[0]
+    a.max_q = q.shape[0] if max_q is None else int(max_q)
+    a.batch = 1
+    if q_offsets is not None:
+        a.batch = max(0, q_offsets.numel() - 1)
+        a.q_offsets = _device_array(q_offsets, "q_offsets", torch.int32, q.device, (a.batch + 1,))
+    return a
+
+
+def _packed_args(q, k, v, q_offsets, k_offsets, max_q, max_k, scale, causal, window, sinks):
+    a = _attention_args(q, k.shape[1] if isinstance(k, torch.Tensor) and k.dim() == 3 else 0, q_offsets, max_q, scale, causal, window, sinks)
+    a.k = _rows(k, "k", q)
+    a.v = _rows(v, "v", q, k.shape[1], k.shape[0])
+    a.total_k = k.shape[0]
+    a.max_k = k.shape[0] if max_k is None else int(max_k)
+    if (q_offsets is None) != (k_offsets is None):
+        raise ValueError("q_offsets and k_offsets are given both or neither")
+    if k_offsets is not None:
+        a.k_offsets = _device_array(k_offsets, "k_offsets", torch.int32, q.device, (a.batch + 1,))
+    return a
+
+
+def _workspace(call, a, device):
+    need = int(call(ctypes.byref(a)))
+    if need < 0:
+        _check(-need)
+    return (torch.empty(need, dtype=torch.uint8, device=device) if need else None), need
+
+
+def attention(q, k, v, q_offsets=None, k_offsets=None, max_q=None, max_k=None, scale=None, causal=True, window=0, sinks=0, out=None,
+              lse=None, stream=None):
+    """f3m_attention: o_i = sum_j w_ij v_j, w_ij = exp(scale q_i.k_j) over its sum; returns (out, lse).
+
+    q (rows, heads, head_dim), k and v (rows, kv_heads, head_dim) hold the sequences behind one another, rows q_offsets[b] ..
+    q_offsets[b + 1] - 1 and the same of k_offsets (int32, on the device; without: one sequence).  max_q and max_k are the longest
+    sequence's (default: all rows; smaller ones make for fewer work items).  causal: token i of nq sees the keys up to
+    nk - nq + i; window > 0: the last `window` of those and the first `sinks`.  scale: 1/sqrt(head_dim) by default.
+    lse (rows, heads) float32: logarithms of the sums, -inf where nothing is visible (and out is 0)."""
+    a = _packed_args(q, k, v, q_offsets, k_offsets, max_q, max_k, scale, causal, window, sinks)
+    with _On(q.device, stream) as on:
+        out = torch.empty(q.shape, dtype=q.dtype, device=q.device) if out is None else out
+        to = _rows(out, "out", q, q.shape[1], q.shape[0])
+        lse = _lse(lse, q.shape[0], q.shape[1], q.device)
+        w, need = _workspace(lib().f3m_attention_workspace, a, q.device)
+        _check(lib().f3m_attention(ctypes.byref(a), ctypes.byref(to), lse.data_ptr() or None, w.data_ptr() if need else None, need, on.handle))
+    return out, lse
+
+
+def attention_grad(dout, q, k, v, out, lse, q_offsets=None, k_offsets=None, max_q=None, max_k=None, scale=None, causal=True, window=0,
+                   sinks=0, dq=None, dk=None, dv=None, stream=None):
+    """f3m_attention_grad: (dq, dk, dv) from the gradient dout of out, with the out and lse of attention() and its arguments."""
+    a = _packed_args(q, k, v, q_offsets, k_offsets, max_q, max_k, scale, causal, window, sinks)
+    g, o = _rows(dout, "dout", q, q.shape[1], q.shape[0]), _rows(out, "out", q, q.shape[1], q.shape[0])
+    if lse is None:
+        raise TypeError("lse must be that of attention()")
+    lse = _lse(lse, q.shape[0], q.shape[1], q.device)
+    with _On(q.device, stream) as on:
+        got = [torch.empty(x.shape, dtype=x.dtype, device=x.device) if y is None else y for x, y in ((q, dq), (k, dk), (v, dv))]
+        to = [_rows(y, name, q, x.shape[1], x.shape[0]) for y, name, x in zip(got, ("dq", "dk", "dv"), (q, k, v))]
+        w, need = _workspace(lib().f3m_attention_grad_workspace, a, q.device)
+        _check(lib().f3m_attention_grad(ctypes.byref(a), ctypes.byref(g), ctypes.byref(o), lse.data_ptr() or None,
+                                        *(ctypes.byref(t) for t in to), w.data_ptr() if need else None, need, on.handle))
+    return tuple(got)
+
+
+class KVCache:
+    """f3m_cache: keys and values in pages, for sequences that grow.  The tensors are the caller's:
+
+    k, v (pages, kv_heads, page_size, head_dim), contiguous, of bfloat16, float16 or float8_e4m3fn; for the last k_exp and v_exp
+    (pages, kv_heads, page_size) uint8, the rows' exponents: a value is code * 2^(byte - 127).  Slot s is row s % page_size of
+    page s // page_size.  KVCache.empty makes the tensors."""
+
+    def __init__(self, k, v, k_exp=None, v_exp=None):
+        if not (isinstance(k, torch.Tensor) and k.is_cuda and k.dim() == 4 and k.dtype in DTYPES):
+            raise TypeError("k must be a device tensor (pages, kv_heads, page_size, head_dim) of bfloat16, float16 or float8_e4m3fn")
+        c = CacheInfo(held=DTYPES[k.dtype], pages=k.shape[0], kv_heads=k.shape[1], page_size=k.shape[2], head_dim=k.shape[3])
+        c.k = _device_array(k, "k", k.dtype, k.device, k.shape)
+        c.v = _device_array(v, "v", k.dtype, k.device, k.shape)
+        if k.dtype == torch.float8_e4m3fn:
+            c.k_exp = _device_array(k_exp, "k_exp", torch.uint8, k.device, k.shape[:3])
+            c.v_exp = _device_array(v_exp, "v_exp", torch.uint8, k.device, k.shape[:3])
+        elif k_exp is not None or v_exp is not None:
+            raise ValueError("k_exp and v_exp belong to 8-bit caches")
+        self.k, self.v, self.k_exp, self.v_exp = k, v, k_exp, v_exp
+        self._c = c
+
+    @classmethod
+    def empty(cls, pages, page_size, kv_heads, head_dim, dtype=torch.float8_e4m3fn, device="cuda"):
+        """a cache of zeros"""
+        def zeros(shape, dtype):
+            return torch.zeros(shape, dtype=torch.uint8, device=device).view(dtype) if dtype == torch.float8_e4m3fn else torch.zeros(shape, dtype=dtype, device=device)
+        shape = (pages, kv_heads, page_size, head_dim)
+        exp = [torch.full(shape[:3], 127, dtype=torch.uint8, device=device) if dtype == torch.float8_e4m3fn else None for _ in range(2)]
+        return cls(zeros(shape, dtype), zeros(shape, dtype), *exp)
+
+    def _move(self, call, k, v, slots, stream):
+        rk, rv = _rows(k, "k"), _rows(v, "v", k, k.shape[1], k.shape[0])
+        if k.shape[1:] != (self._c.kv_heads, self._c.head_dim) or k.device != self.k.device:
+            raise ValueError("k and v must have shape (tokens, kv_heads, head_dim) as the cache, and be on its device")
+        at = _device_array(slots, "slots", torch.int64, self.k.device, (k.shape[0],))
+        with _On(self.k.device, stream) as on:
+            _check(call(ctypes.byref(self._c), DTYPES[k.dtype], ctypes.byref(rk), ctypes.byref(rv), at, k.shape[0], on.handle))
+
+    def write(self, k, v, slots, stream=None):
+        """f3m_cache_write: k, v (tokens, kv_heads, head_dim) to slots (tokens) int64, on the device; slots outside the cache are skipped.
+        No slot may come twice in a call."""
+        self._move(lib().f3m_cache_write, k, v, slots, stream)
+
+    def read(self, slots, dtype=None, k=None, v=None, stream=None):
+        """f3m_cache_read: (k, v) of the slots, of `dtype` (default: bfloat16 from an 8-bit cache, else the cache's); zeros for slots outside"""
+        dtype = (torch.bfloat16 if self._c.held == 2 else self.k.dtype) if dtype is None else dtype
+        shape = (slots.numel(), self._c.kv_heads, self._c.head_dim)
+        with _On(self.k.device, stream) as on:
+            k = torch.empty(shape, dtype=dtype, device=self.k.device) if k is None else k
+            v = torch.empty(shape, dtype=dtype, device=self.k.device) if v is None else v
+            self._move(lib().f3m_cache_read, k, v, slots, on.stream)
+        return k, v
+
+    def attention(self, q, table, lengths, q_offsets=None, max_q=None, max_k=None, scale=None, causal=True, window=0, sinks=0, out=None,
+                  lse=None, stream=None):
+        """f3m_cache_attention: attention() of new tokens q over the sequences of the cache, their own keys included; returns (out, lse).
+
+        Key j of sequence b lies in page table[b, j // page_size] (int32, on the device), j < lengths[b] (int32, on the device).
+        q_offsets as for attention(); without, every sequence has the same number of new tokens (rows of q / sequences).
+        max_k: the longest length (default: what the table has room for)."""
+        if not (isinstance(table, torch.Tensor) and table.is_cuda and table.dtype == torch.int32 and table.dim() == 2 and table.device == self.k.device):
+            raise TypeError("table must be an int32 tensor (sequences, pages) on the cache's device")
+        if table.numel() and table.shape[1] > 1 and table.stride(1) != 1 or table.stride(0) < table.shape[1] and table.shape[0] > 1:
+            raise ValueError("table must be contiguous along the pages")
+        batch = table.shape[0]
+        _rows(q, "q")
+        with _On(self.k.device, stream) as on:
+            if q_offsets is None:
+                if q.shape[0] % max(1, batch):
+                    raise ValueError("without q_offsets all sequences have the same number of new tokens")
+                each = q.shape[0] // max(1, batch)
+                q_offsets = torch.arange(batch + 1, dtype=torch.int32, device=self.k.device).mul_(each)
+                max_q = each if max_q is None else max_q
+            a = _attention_args(q, self._c.kv_heads, q_offsets, max_q, scale, causal, window, sinks)
+            if a.batch != batch or q.device != self.k.device:
+                raise ValueError("q_offsets must have one entry more than the table has rows, and q must be on the cache's device")
+            ln = _device_array(lengths, "lengths", torch.int32, self.k.device, (batch,))
+            a.max_k = min(table.shape[1] * self._c.page_size, 2 ** 31 - 65537) if max_k is None else int(max_k)
+            out = torch.empty(q.shape, dtype=q.dtype, device=q.device) if out is None else out
+            to = _rows(out, "out", q, q.shape[1], q.shape[0])
+            lse = _lse(lse, q.shape[0], q.shape[1], q.device)
+            w, need = _workspace(lib().f3m_attention_workspace, a, q.device)
+            _check(lib().f3m_cache_attention(ctypes.byref(self._c), ctypes.byref(a), table.data_ptr() if table.numel() else None,
+                                             max(table.stride(0), table.shape[1]), table.shape[1], ln, ctypes.byref(to), lse.data_ptr() or None,
+                                             w.data_ptr() if need else None, need, on.handle))
+        return out, lse

@@ -1,0 +1,274 @@
+"""KVCache: writing, reading back and attention over pages, against the definition in 64 bits (attention_util.py)."""
+import numpy as np
+import pytest
+import torch
+
+import attention_util as au
+from paper_2202_01085_amd import f3m
+
+pytestmark = pytest.mark.gpu
+DEV = "cuda:0"
+BF, HF, E8 = torch.bfloat16, torch.float16, torch.float8_e4m3fn
+
+
+def normal(shape, seed, type, size=1.0):
+    g = torch.Generator().manual_seed(seed)
+    return (torch.randn(shape, generator=g) * size).to(type)
+
+
+def quantised(x):
+    """(codes as fp64, exponent bytes) of rows x (fp64, finite values and others), from the rule alone"""
+    finite = torch.isfinite(x)
+    top = torch.where(finite, x.abs(), torch.zeros_like(x)).amax(-1)
+    byte = torch.empty(top.shape, dtype=torch.int64)
+    for i, t in enumerate(top.flatten().tolist()):
+        e = -126
+        while t > 448.0 * 2.0 ** e:
+            e += 1
+        byte.view(-1)[i] = 127 if t == 0 else e + 127
+    y = x / torch.exp2(byte.double() - 127)[..., None]
+    _, e = torch.frexp(torch.where(finite, y, torch.zeros_like(y)))
+    step = torch.exp2((e - 4).clamp(min=-9).double())
+    return torch.where(finite, torch.round(y / step) * step, torch.full_like(y, torch.nan)), byte
+
+
+@pytest.mark.parametrize("type", [BF, HF])
+@pytest.mark.parametrize("D,heads,page", [(16, 1, 8), (32, 3, 16), (64, 2, 1024), (80, 2, 32), (128, 4, 64)])
+def test_write_and_read_8_bits(type, D, heads, page):
+    T, pages = 77, 2 + 200 // page
+    k, v = normal((T, heads, D), 1, type), normal((T, heads, D), 2, type, 30.0)
+    k[0] = 0
+    k[1, :, 3] = 300.0
+    k[2, :, 5] = torch.finfo(type).max if type == BF else 60000.0
+    k[3] = torch.finfo(type).tiny
+    k[4, :, 0], k[4, :, 1], k[4, :, 2] = float("nan"), float("inf"), -float("inf")
+    k[5] = 448.0
+    k[6] = 449.0 if type == HF else 450.0
+    v[7] = torch.finfo(type).smallest_normal * torch.finfo(type).eps      # the smallest number of the type
+    slots = torch.randperm(pages * page, generator=torch.Generator().manual_seed(3))[:T]
+    slots[10], slots[11], slots[12] = -1, pages * page, -2 ** 60
+    c = f3m.KVCache.empty(pages, page, heads, D, device=DEV)
+    c.write(k.to(DEV), v.to(DEV), slots.to(DEV))
+    k2, v2 = c.read(slots.to(DEV), dtype=type)
+    some = (slots >= 0) & (slots < pages * page)
+    left = torch.ones(pages * page, dtype=torch.bool)
+    left[slots[some]] = False
+    for x, back, codes, exps in ((k, k2, c.k, c.k_exp), (v, v2, c.v, c.v_exp)):
+        q, byte = quantised(x.double())
+        at = slots[some]
+        got, gote = codes.cpu().permute(0, 2, 1, 3).reshape(-1, heads, D).double(), exps.cpu().permute(0, 2, 1).reshape(-1, heads).long()
+        assert torch.equal(gote[at], byte[some])
+        assert torch.equal(torch.nan_to_num(got[at], nan=1e9), torch.nan_to_num(q[some], nan=1e9))
+        assert not got[left].any() and (gote[left] == 127).all()
+        want = (q * torch.exp2(byte.double() - 127)[..., None]).to(type)
+        back = back.cpu()
+        assert torch.equal(torch.nan_to_num(back[some], nan=7.0), torch.nan_to_num(want[some], nan=7.0))
+        assert not back[~some].any()
+
+
+@pytest.mark.parametrize("type", [BF, HF])
+def test_write_and_read_16_bits(type):
+    c = f3m.KVCache.empty(9, 16, 2, 40, dtype=type, device=DEV)
+    x = normal((30, 4, 48), 1, type).to(DEV)
+    k, v = x[:, :2, :40], x[:, 2:, 8:]
+    slots = torch.randperm(144, device=DEV)[:30]
+    c.write(k, v, slots)
+    back = c.read(slots)
+    assert torch.equal(back[0], k) and torch.equal(back[1], v)
+    wide = torch.zeros((30, 2, 96), dtype=type, device=DEV)
+    c.read(slots, k=wide[:, :, :40], v=wide[:, :, 48:88])
+    assert torch.equal(wide[:, :, :40], k) and torch.equal(wide[:, :, 48:88], v) and not wide[:, :, 40:48].any()
+    c.write(k[:0], v[:0], slots[:0])
+    assert c.read(slots[:0])[0].shape == (0, 2, 40)
+
+
+def filled(type, held, lengths, heads, D, page, seed, extra=3):
+    """a cache with sequences of these lengths in shuffled pages, NaN in what no key lies in; the table; the packed keys and values"""
+    g = torch.Generator().manual_seed(seed)
+    counts = [-(-n // page) for n in lengths]
+    pages = sum(counts) + extra
+    order = torch.randperm(pages, generator=g)
+    table = torch.full((len(lengths), max(counts + [1]) + 1), -1, dtype=torch.int32)
+    c = f3m.KVCache.empty(pages, page, heads, D, dtype=held, device=DEV)
+    (c.k.view(torch.uint8) if held == E8 else c.k).fill_(0x7f if held == E8 else float("nan"))
+    (c.v.view(torch.uint8) if held == E8 else c.v).fill_(0x7f if held == E8 else float("nan"))
+    total, at = sum(lengths), 0
+    k, v = normal((total, heads, D), seed + 1, type), normal((total, heads, D), seed + 2, type)
+    slots = []
+    for b, n in enumerate(lengths):
+        table[b, :counts[b]] = order[at:at + counts[b]].int()
+        at += counts[b]
+        j = torch.arange(n)
+        slots.append(table[b, j // page].long() * page + j % page)
+    slots = torch.cat(slots).to(DEV)
+    c.write(k.to(DEV), v.to(DEV), slots)
+    k, v = (x.cpu() for x in c.read(slots, dtype=type))      # what the cache stands for
+    return c, table.to(DEV), k, v
+
+
+def check(type, held, news, lengths, Hq, Hk, D, page, window=0, sinks=0, seed=1, max_k=None):
+    print("cache attention", type, held, news, lengths, Hq, Hk, D, page, window, sinks, flush=True)
+    c, table, k, v = filled(type, held, lengths, Hk, D, page, seed)
+    qo, ko = au.offsets(news), au.offsets(lengths)
+    q = normal((qo[-1], Hq, D), seed + 5, type)
+    scale = 1.0 / D ** 0.5
+    want = au.batch(q, k, v, qo, ko, float(np.float32(scale)), True, window, sinks)
+    ln = torch.tensor(lengths, dtype=torch.int32, device=DEV)
+    out, lse = c.attention(q.to(DEV), table, ln, torch.tensor(qo, dtype=torch.int32, device=DEV), max_q=max(news), max_k=max_k, window=window, sinks=sinks)
+    au.close(lse, want, "lse")
+    au.close(out, want, "out")
+
+
+@pytest.mark.parametrize("type,held", [(BF, E8), (HF, E8), (BF, BF), (HF, HF)])
+@pytest.mark.parametrize("D,page", [(32, 8), (64, 16), (80, 32), (128, 64), (128, 16)])
+def test_single_tokens(type, held, D, page):
+    check(type, held, [1, 1, 1, 1, 1], [1, 300, 33, 64, 1029], 8, 2, D, page, seed=D)
+
+
+@pytest.mark.parametrize("type,held", [(BF, E8), (HF, HF)])
+@pytest.mark.parametrize("window,sinks", [(0, 0), (1, 0), (50, 4), (700, 40)])
+def test_chunks(type, held, window, sinks):
+    check(type, held, [130, 1, 0, 17, 64], [500, 900, 40, 17, 70], 6, 2, 128, 16, window, sinks, seed=window)
+    check(type, held, [7, 9], [1000, 13], 4, 4, 64, 128, window, sinks, seed=window + 1)
+
+
+@pytest.mark.parametrize("news,lengths,Hq,Hk", [([1], [30000], 8, 1), ([1, 1], [9000, 12], 2, 2), ([5], [12000], 16, 1), ([200], [9000], 4, 4)])
+def test_long_texts(news, lengths, Hq, Hk):
+    check(BF, E8, news, lengths, Hq, Hk, 128, 16, seed=3, max_k=max(lengths))
+    check(BF, BF, news, lengths, Hq, Hk, 64, 32, window=5000, sinks=2, seed=4)
+
+
+def test_empty_sequences_and_more_tokens_than_keys():
+    check(BF, E8, [3, 1, 5], [0, 1, 2], 4, 2, 64, 16)
+
+
+def test_bad_pages_hide_their_keys():
+    """page numbers outside the cache: the keys in them are hidden, the others as before, also where all of a row's are"""
+    D, page, n = 64, 16, 200
+    c, table, k, v = filled(BF, E8, [n, n], 2, D, page, 9)
+    bad = table.clone()
+    bad[0, 3], bad[0, 5], bad[1, :] = -7, 2 ** 30, 10 ** 9
+    ln = torch.tensor([n, n], dtype=torch.int32, device=DEV)
+    for new in (1, 70):
+        q = normal((2 * new, 4, D), 4, BF)
+        out, lse = c.attention(q.to(DEV), bad, ln)
+        for i, (scale, rows) in enumerate(((0.125, slice(0, new)),)):
+            keep = torch.ones(n, dtype=torch.bool)
+            keep[48:64] = keep[80:96] = False
+            seen = au.visible(new, n, True, 0, 0) & keep
+            for h in range(4):
+                r = au.sequence(q[rows, h].double(), k[:n, h // 2].double(), v[:n, h // 2].double(), seen, scale, 2.0 ** -8, False)
+                au.close(out[rows, h], r, "out")
+                au.close(lse[rows, h], r, "lse")
+        assert not out[new:].any() and (lse[new:] == -float("inf")).all()
+    # lengths past the table's room are cut, negative ones are 0
+    q = normal((2, 4, D), 5, BF).to(DEV)
+    out, lse = c.attention(q, table, torch.tensor([2 ** 31 - 1, -4], dtype=torch.int32, device=DEV))
+    assert not out[1].any() and (lse[1] == -float("inf")).all()
+
+
+def test_nan_in_the_cache_reaches_only_tokens_that_see_it():
+    D, page, n = 128, 16, 300
+    c, table, k, v = filled(BF, E8, [n], 1, D, page, 11)
+    slot = int(table[0, 250 // page]) * page + 250 % page
+    odd = normal((1, 1, D), 3, BF)
+    odd[0, 0, 7] = float("nan")
+    c.write(k[250:251].to(DEV), odd.to(DEV), torch.tensor([slot], device=DEV))
+    q = normal((100, 2, D), 4, BF)      # positions 200 .. 299
+    out, lse = c.attention(q.to(DEV), table, torch.tensor([n], dtype=torch.int32, device=DEV), scale=0.1)
+    assert torch.isfinite(out[:50]).all() and torch.isnan(out[50:, :, 7]).all() and torch.isfinite(lse).all()
+
+
+def test_a_text_goes_through_the_cache():
+    """the operators together, as a server uses them: a prompt attended to as a whole and written, then chunks and single tokens written and
+    attended to; every step equals attention over all tokens so far, as the cache holds them; the steps replayed from a graph too"""
+    Hq, Hk, D, page, how = 4, 2, 64, 16, dict(window=60, sinks=4)
+    c = f3m.KVCache.empty(40, page, Hk, D, device=DEV)
+    total = 300
+    q, k, v = (normal((total, h, D), 30 + i, BF).to(DEV) for i, h in enumerate((Hq, Hk, Hk)))
+    table = torch.randperm(40, generator=torch.Generator().manual_seed(1)).int()[None, :20].contiguous().to(DEV)
+    j = torch.arange(total, device=DEV)
+    slots = table[0, j // page].long() * page + j % page
+    c.write(k, v, slots)
+    kq, vq = c.read(slots)
+    full, full_lse = f3m.attention(q, kq, vq, **how)
+    c2 = f3m.KVCache.empty(40, page, Hk, D, device=DEV)
+    at = 0
+    for step in (130, 70, 1, 1, 33, 1):
+        rows = slice(at, at + step)
+        c2.write(k[rows], v[rows], slots[rows])
+        at += step
+        out, lse = c2.attention(q[rows], table, torch.tensor([at], dtype=torch.int32, device=DEV), **how)
+        # the same sums in another order: two roundings of the result and of the weights, 2^-8 each of values of about 1
+        assert (lse - full_lse[rows]).abs().max() < 1e-5
+        assert (out.float() - full[rows].float()).abs().max() <= 4 * 2.0 ** -8 * full.abs().max()
+    # the rest token by token from one graph: the slot, the length and the token are inputs
+    qs, ks, vs = (torch.empty((1, h, D), dtype=BF, device=DEV) for h in (Hq, Hk, Hk))
+    slot, length = torch.zeros(1, dtype=torch.int64, device=DEV), torch.zeros(1, dtype=torch.int32, device=DEV)
+    slot.fill_(-1)
+    g = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(g):
+        c2.write(ks, vs, slot)
+        out, lse = c2.attention(qs, table, length, **how)
+    for t in range(at, at + 20):
+        qs.copy_(q[t:t + 1])
+        ks.copy_(k[t:t + 1])
+        vs.copy_(v[t:t + 1])
+        slot.copy_(slots[t:t + 1])
+        length.fill_(t + 1)
+        g.replay()
+        torch.cuda.synchronize()
+        assert (lse - full_lse[t:t + 1]).abs().max() < 1e-5
+        assert (out.float() - full[t:t + 1].float()).abs().max() <= 4 * 2.0 ** -8 * full.abs().max()
+    torch.cuda.synchronize()
+    assert torch.equal(c2.k.view(torch.uint8)[table[0, :16].long()], c.k.view(torch.uint8)[table[0, :16].long()])
+
+
+def test_offsets_past_32_bits():
+    """a cache of more than 2^32 values: a sequence in its last pages"""
+    D, heads, page = 128, 8, 64
+    pages = 2 ** 32 // (D * heads * page) + 20
+    c = f3m.KVCache.empty(pages, page, heads, D, device=DEV)
+    n = 150
+    k, v = normal((n, heads, D), 1, BF), normal((n, heads, D), 2, BF)
+    table = torch.tensor([[pages - 1, pages - 3, pages - 2]], dtype=torch.int32)
+    j = torch.arange(n)
+    slots = (table[0, j // page].long() * page + j % page).to(DEV)
+    c.write(k.to(DEV), v.to(DEV), slots)
+    k, v = (x.cpu() for x in c.read(slots))
+    q = normal((1, 8, D), 3, BF)
+    out, lse = c.attention(q.to(DEV), table.to(DEV), torch.tensor([n], dtype=torch.int32, device=DEV), scale=0.125)
+    want = au.batch(q, k, v, [0, 1], [0, n], 0.125)
+    au.close(out, want, "out")
+    au.close(lse, want, "lse")
+
+
+def test_binding_refuses():
+    c = f3m.KVCache.empty(4, 16, 2, 64, device=DEV)
+    x = torch.zeros((3, 2, 64), dtype=BF, device=DEV)
+    slots = torch.arange(3, device=DEV)
+    with pytest.raises(TypeError):
+        c.write(x, x, slots.int())
+    with pytest.raises(ValueError):
+        c.write(x, x, slots[:2])
+    with pytest.raises(ValueError):
+        c.write(x[:, :1], x[:, :1], slots)
+    with pytest.raises(TypeError):
+        f3m.KVCache(c.k.view(torch.uint8), c.v, c.k_exp, c.v_exp)
+    with pytest.raises(TypeError):
+        f3m.KVCache(c.k, c.v)
+    with pytest.raises(f3m.F3MError):
+        f3m.KVCache.empty(4, 12, 2, 64, device=DEV).write(x, x, slots)          # page_size
+    with pytest.raises(f3m.F3MError):
+        f3m.KVCache.empty(4, 16, 2, 64, dtype=HF, device=DEV).write(x, x, slots)
+    table, ln = torch.zeros((1, 2), dtype=torch.int32, device=DEV), torch.ones(1, dtype=torch.int32, device=DEV)
+    with pytest.raises(TypeError):
+        c.attention(x, table.long(), ln)
+    with pytest.raises(ValueError):
+        c.attention(x, table, ln, torch.zeros(3, dtype=torch.int32, device=DEV))
+    with pytest.raises(f3m.F3MError):
+        c.attention(torch.zeros((1, 3, 64), dtype=BF, device=DEV), table, ln)   # heads not a multiple
+    with pytest.raises(f3m.F3MError):
+        c.attention(torch.zeros((1, 2, 32), dtype=BF, device=DEV), table, ln)   # head_dim
+    with pytest.raises(f3m.F3MError):
+        c.attention(x, table, ln, scale=float("nan"))
