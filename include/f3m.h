@@ -299,8 +299,8 @@ f3m_status f3m_cg_solve(f3m_plan_t *plan, float lambda, const float *b, float *x
  * least the same elements of o NaN or infinite, one in k, q or dout all that depends on the pair.
  * Offsets and lengths are read on the device and not checked by the host: such as lie outside the tensors or fall are
  * cut to what exists, no access leaves the tensors.
- * Limits: head_dim a multiple of 8 up to 128; data 16-byte aligned, strides multiples of 8 values; fewer than
- * 2^31 - 65536 rows.
+ * Limits: head_dim a multiple of 8 up to 128; data 16-byte aligned, strides multiples of 8 values, those between rows
+ * below 2^22; fewer than 2^31 - 65536 rows.
  * Every call is asynchronous on `stream` and allocates nothing; the caller brings the workspace (the *_workspace calls
  * say how many bytes) and gives each call that may run at the same time its own.  Any call may be captured into a HIP
  * graph.  Sums are made in a fixed order: results repeat bit for bit.

@@ -85,10 +85,10 @@ f3m_status check_attention(const f3m_attention_args *p, bool paged = false) {
 }
 
 f3m_status check_rows(const f3m_rows &r, int64_t rows, const char *name) {
-    (void)rows;
     if (!r.data) return set_error(F3M_ERR_INVALID_ARG, std::string(name) + " is null");
     if ((uintptr_t)r.data % 16 || r.row % 8 || r.head % 8 || r.row < 0 || r.head < 0)
         return set_error(F3M_ERR_INVALID_ARG, std::string(name) + ": data must be 16-byte aligned, strides multiples of 8 values and >= 0");
+    if (rows > 1 && r.row >= 1 << 22) return set_error(F3M_ERR_UNSUPPORTED, std::string(name) + ": rows 2^22 values apart or more are not supported");
     return F3M_OK;
 }
 
@@ -354,7 +354,7 @@ int64_t f3m_attention_workspace(const f3m_attention_args *args) {
 
 int64_t f3m_attention_grad_workspace(const f3m_attention_args *args) {
     f3m_status st = check_attention(args);
-    return st != F3M_OK ? -(int64_t)st : f3m::attend_grad_workspace(attend_args(*args));
+    return st != F3M_OK ? -(int64_t)st : f3m::attend_grad_workspace(attend_args(*args), args->max_k);
 }
 
 f3m_status f3m_attention(const f3m_attention_args *args, const f3m_rows *out, float *lse, void *workspace, int64_t workspace_bytes,
@@ -396,7 +396,7 @@ f3m_status f3m_attention_grad(const f3m_attention_args *args, const f3m_rows *do
     }
     if (st != F3M_OK) return st;
     f3m::AttendArgs a = attend_args(*args);
-    st = check_workspace(workspace, workspace_bytes, f3m::attend_grad_workspace(a));
+    st = check_workspace(workspace, workspace_bytes, f3m::attend_grad_workspace(a, args->max_k));
     if (st != F3M_OK) return st;
     if (args->total_q > 0) {
         a.dout = rows_of(*dout);

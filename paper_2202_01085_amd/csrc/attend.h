@@ -37,7 +37,8 @@ struct AttendArgs {
     float *part_out, *part_lse;               // (parts, rows of q, heads, dim) and (parts, rows of q, heads)
     // gradient
     Rows dout, dq, dk, dv;
-    float2 *stat;                             // (rows of q, heads): log2 of the row's sum (inf: empty row), dO.O
+    float *stat;                              // (2, heads, rows of q): log2 of the row's sum (inf: empty row), dO.O
+    int split;                                // key tiles of a group that may be cut into parts; chunk is in row tiles there
 };
 
 using s16x4 = __attribute__((ext_vector_type(4))) short;
@@ -89,7 +90,7 @@ struct F16 {
 int64_t attend_workspace(AttendArgs a, int64_t max_k);
 void run_attend(AttendArgs a, int64_t max_k, bool f16, bool e8, void *workspace, hipStream_t st);
 int64_t attend_blocks(AttendArgs &a, int64_t items);
-int64_t attend_grad_workspace(const AttendArgs &a);
+int64_t attend_grad_workspace(AttendArgs a, int64_t max_k);
 void run_attend_grad(AttendArgs a, int64_t max_k, bool f16, void *workspace, hipStream_t st);
 // cache.hip
 void run_cache_rows(const f3m_cache &c, bool f16, const int64_t *slot, int64_t tokens, const f3m_rows &k, const f3m_rows &v, bool write,
@@ -188,7 +189,17 @@ __device__ __forceinline__ Limits limits_of(const AttendArgs &a, const Sequence 
     const int pos = s.nk - s.nq + token;
     return {a.window && pos >= a.window ? pos - a.window + 1 : 0, pos + 1};
 }
-__device__ __forceinline__ bool sees(const Limits &m, int sinks, int key) { return key < m.hi && (key >= m.lo || key < sinks); }
+
+// bits of the keys of a tile (bit r: key0 + r) that a row sees
+__device__ __forceinline__ uint64_t below(int n) { return n >= 64 ? ~0ull : n <= 0 ? 0ull : (1ull << n) - 1; }
+__device__ __forceinline__ uint64_t seen_bits(const Limits &m, int sinks, int key0) {
+    return below(m.hi - key0) & (~below(m.lo - key0) | below(sinks - key0));
+}
+// x where bit `at` of the word is set, else y
+__device__ __forceinline__ float pick(uint32_t bits, int at, float x, float y) {
+    const uint32_t t = (uint32_t)((int32_t)(bits << (31 - at)) >> 31);
+    return __builtin_bit_cast(float, (t & __builtin_bit_cast(uint32_t, x)) | (~t & __builtin_bit_cast(uint32_t, y)));
+}
 
 // key tiles of N rows that rows with limits from `first` to `last` see: the tiles of the sinks, then those of the window
 struct Tiles {
@@ -246,6 +257,78 @@ __device__ __forceinline__ Place place_of(const AttendArgs &a, const Sequence &s
     p.exp_at = (((int64_t)(p.ok ? page : 0) * a.kv_heads + hk) << a.page_shift) + (j & ((1 << a.page_shift) - 1));
     p.at = p.exp_at * a.dim;
     return p;
+}
+
+// ---- tiles straight from memory to LDS ----
+// 16 bytes to a lane, 1 KB to an instruction, in the order of LDS: lane i's bytes go to `lds` + 16 i.  So which piece of which row a lane
+// reads follows from where it has to lie (tile_at).  Written out, because the compiler, which cannot tell the tiles apart, would wait
+// for the loads before every transposing read of another tile; nothing comes back in registers, and arrived() waits for them.
+__device__ __forceinline__ u32x4 buffer_of(const char *p, int64_t bytes) {   // reads past `bytes` give zeros
+    const uint64_t at = (uint64_t)p;
+    return (u32x4){(uint32_t)__builtin_amdgcn_readfirstlane((uint32_t)at), (uint32_t)__builtin_amdgcn_readfirstlane((uint32_t)(at >> 32)),
+                   (uint32_t)__builtin_amdgcn_readfirstlane((uint32_t)min(max(bytes, (int64_t)0), (int64_t)0x7fffffff)), 0x00020000u};
+}
+__device__ __forceinline__ void to_lds(u32x4 buffer, uint32_t lane_offset, uint32_t offset, uint32_t lds) {
+    asm volatile("s_mov_b32 m0, %0\n\tbuffer_load_dwordx4 %1, %2, %3 offen lds" ::"s"(__builtin_amdgcn_readfirstlane(lds)), "v"(lane_offset),
+                 "s"(buffer), "s"(__builtin_amdgcn_readfirstlane(offset)) : "memory");
+}
+__device__ __forceinline__ void to_lds(const char *p, uint32_t lds) {
+    asm volatile("s_mov_b32 m0, %0\n\tglobal_load_lds_dwordx4 %1, off" ::"s"(__builtin_amdgcn_readfirstlane(lds)), "v"(p) : "memory");
+}
+__device__ __forceinline__ void word_to_lds(const float *p, uint32_t lds) {   // 4 bytes to a lane
+    asm volatile("s_mov_b32 m0, %0\n\tglobal_load_lds_dword %1, off" ::"s"(__builtin_amdgcn_readfirstlane(lds)), "v"(p) : "memory");
+}
+__device__ __forceinline__ void arrived() { asm volatile("s_waitcnt vmcnt(0)" ::: "memory"); }
+using lds_short = __attribute__((address_space(3))) short;
+__device__ __forceinline__ uint32_t lds_address(const short *p) { return (uint32_t)(uintptr_t)(const lds_short *)p; }
+
+// Tiles of N rows from two tensors (keys and values, say) with fixed strides, for a block of four waves
+template <class T, int DP, int N> struct Tile2 {
+    static constexpr int PIECES = DP / 8, RPI = 64 / PIECES, STEP = 4 * RPI, COUNT = (N + STEP - 1) / STEP;   // rows to an instruction, of four waves
+    uint32_t off[2];           // the lane's bytes within the wave's first instruction
+    int row, piece;            // the lane's row there, its piece
+    const char *base[2];       // row 0
+    int64_t stride[2];
+
+    __device__ void start(const char *x, int64_t xrow, const char *y, int64_t yrow, int dim, int wave, int lane) {
+        row = wave * RPI + lane / PIECES;
+        piece = (lane % PIECES) ^ piece_swap<DP>(row);
+        base[0] = x;
+        base[1] = y;
+        stride[0] = 2 * xrow;
+        stride[1] = 2 * yrow;
+#pragma unroll
+        for (int w = 0; w < 2; ++w)                        // zeros where the tile is wider than the head
+            off[w] = piece * 8 >= dim ? 0x7fffff00u : (uint32_t)(row * (int)stride[w] + piece * 16);
+    }
+    // rows from row0 on; rows from `end` on give zeros
+    __device__ void issue(int row0, int end, int dim, const short *tx, const short *ty, int wave) const {
+        if (N < STEP && wave * RPI >= N) return;
+#pragma unroll
+        for (int w = 0; w < 2; ++w) {
+            const u32x4 buffer = buffer_of(base[w] + row0 * stride[w], (end - 1 - row0) * stride[w] + 2 * dim);
+            const uint32_t lds = lds_address(w ? ty : tx) + wave * 1024;
+#pragma unroll
+            for (int c = 0; c < COUNT; ++c) to_lds(buffer, off[w], (uint32_t)(STEP * c * (int)stride[w]), lds + 4096 * c);
+        }
+    }
+};
+// infinities and NaN of a tile become 0; bits of the rows that had one (a wave's)
+template <class T, int DP, int N> __device__ __forceinline__ uint64_t clean_tile(short *tile, int tid) {
+    constexpr int PIECES = DP / 8;
+    uint64_t odd = 0;
+#pragma unroll
+    for (int at = tid; at < N * PIECES; at += 256) {
+        const u32x4 w = *(const u32x4 *)(tile + 8 * at);
+        if (any_odd<T>(w)) {
+            *(u32x4 *)(tile + 8 * at) = cleaned<T>(w);
+            odd |= 1ull << (at / PIECES);
+        }
+    }
+    if (!__any(odd != 0)) return 0;
+#pragma unroll 1
+    for (int by = 32; by > 0; by >>= 1) odd |= __shfl_xor((unsigned long long)odd, by);
+    return odd;
 }
 
 // 16 bytes of zeros where the tile is wider than the head

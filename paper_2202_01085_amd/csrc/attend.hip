@@ -92,14 +92,14 @@ __device__ __forceinline__ uint64_t good_pages(const AttendArgs &a, const Sequen
     return __ballot(page >= 0 && page < a.pages);
 }
 
-// what a wave carries from tile to tile
+// What a wave carries from tile to tile, for its 32 rows
 template <class T, int DP> struct Rows32 {
     static constexpr int KS = DP / 16, DB = DP / 32;
     static constexpr float LIFT = T::narrow ? 7.f : 0.f;   // log2 of the factor that weights are held with
     s16x8 q[KS];
     f32x16 o[DB];
-    float m, l;        // largest score so far as used, sum of the weights (of this lane's half of the keys) times 2^LIFT
-    float spoil;       // 0, or NaN once the row (in this lane's half) has seen an odd v
+    float m, l;     // largest score so far as used, sum of the weights (of this lane's half of the keys) times 2^LIFT
+    float spoil;    // 0, or NaN once the row (in this lane's half) has seen an odd v
 
     __device__ void start(const AttendArgs &a, const char *base, int64_t at, int lane) {
 #pragma unroll
@@ -114,26 +114,20 @@ template <class T, int DP> struct Rows32 {
     // NB blocks of 32 keys from key0 on, whose rows lie in LDS from row 0 on.  edge: the mask cuts the tile for some row, or `good` (rows
     // in pages of the cache) or `odd` (rows whose infinities or NaN in v are cleaned away) say something
     template <int NB>
-    __device__ void step(const short *kt, const short *vt, int key0, bool edge, uint64_t good, uint64_t odd, const Limits &mine, int sinks, float c, int lane) {
+    __device__ __forceinline__ void step(const short *kt, const short *vt, int key0, bool edge, uint64_t good, uint64_t odd, const Limits &mine, int sinks,
+                                         float c, int lane) {
         f32x16 s[NB];
 #pragma unroll
-        for (int kb = 0; kb < NB; ++kb) {
-            s[kb] = (f32x16)0.f;
+        for (int kb = 0; kb < NB; ++kb)
 #pragma unroll
-            for (int ks = 0; ks < KS; ++ks) s[kb] = T::mma(frag_r<DP>(kt, 32 * kb, ks, lane), q[ks], s[kb]);
-        }
+            for (int ks = 0; ks < KS; ++ks) s[kb] = T::mma(frag_r<DP>(kt, 32 * kb, ks, lane), q[ks], ks ? s[kb] : (f32x16)0.f);
         if (edge) {
-            bool spoilt = false;
+            const uint64_t seen = seen_bits(mine, sinks, key0) & good, bits = seen >> (4 * (lane >> 5));
+            if (seen & odd) spoil = __builtin_nanf("");
 #pragma unroll
             for (int kb = 0; kb < NB; ++kb)
 #pragma unroll
-                for (int i = 0; i < 16; ++i) {
-                    const int r = 32 * kb + c_row(i, lane);
-                    const bool seen = sees(mine, sinks, key0 + r) && ((good >> r) & 1);
-                    s[kb][i] = seen ? s[kb][i] : NO_KEY;
-                    spoilt |= seen && ((odd >> r) & 1);
-                }
-            spoil = spoilt ? __builtin_nanf("") : spoil;
+                for (int i = 0; i < 16; ++i) s[kb][i] = pick((uint32_t)(bits >> (32 * kb)), c_row(i, 0), s[kb][i], NO_KEY);
         }
         float top = s[0][0];
 #pragma unroll
@@ -141,7 +135,7 @@ template <class T, int DP> struct Rows32 {
 #pragma unroll
             for (int i = 0; i < 16; ++i) top = fmaxf(top, s[kb][i]);
         top = both_halves_max(top);
-        if (__any((top - m) * c > GROW)) {         // m = -inf: the difference is inf, or NaN while nothing is visible
+        if (__any((top - m) * c > GROW)) {       // m = -inf: the difference is inf, or NaN while nothing is visible
             const float now = fmaxf(m, top), by = m == now ? 1.f : __builtin_amdgcn_exp2f((m - now) * c);
             m = now;
             l *= by;
@@ -172,21 +166,54 @@ template <class T, int DP> struct Rows32 {
     __device__ float lse(float all, float c) const { return all > 0.f ? (m * c - LIFT + __builtin_amdgcn_logf(all)) * LN2 : all == all ? NO_KEY : all; }
 };
 
-// Many rows: a work item is 128 rows of one group, the four waves share tiles of 64 keys.  Bound by the matrix cores and by
-// what LDS delivers to them (one operand of each product comes from there).
+// Tiles of K and V straight to LDS, from rows of a tensor or from pages of a 16-bit cache
+template <class T, int DP> struct Direct : Tile2<T, DP, KT> {
+    using Base = Tile2<T, DP, KT>;
+    int pages[Base::COUNT];    // of the next tile's rows
+
+    __device__ void start(const AttendArgs &a, const Sequence &s, int hk, int wave, int lane) {
+        if (a.table) Base::start(a.k.p, 0, a.v.p, 0, a.dim, wave, lane);
+        else Base::start(a.k.p + 2 * ((int64_t)s.k0 * a.k.row + (int64_t)hk * a.k.head), a.k.row, a.v.p + 2 * ((int64_t)s.k0 * a.v.row + (int64_t)hk * a.v.head), a.v.row, a.dim, wave, lane);
+    }
+    __device__ void look(const AttendArgs &a, const Sequence &s, int b, int key0) {
+        if (!a.table) return;
+#pragma unroll
+        for (int c = 0; c < Base::COUNT; ++c) {
+            const int j = min(key0 + this->row + Base::STEP * c, s.nk - 1), page = a.table[(int64_t)b * a.table_row + (j >> a.page_shift)];
+            pages[c] = page >= 0 && page < a.pages ? page : 0;
+        }
+    }
+    __device__ void issue(const AttendArgs &a, const Sequence &s, int hk, int key0, const short *kt, const short *vt, int wave) const {
+        if (!a.table) {
+            Base::issue(key0, s.nk, a.dim, kt, vt, wave);
+            return;
+        }
+#pragma unroll
+        for (int c = 0; c < Base::COUNT; ++c) {
+            const int j = min(key0 + this->row + Base::STEP * c, s.nk - 1), piece = this->piece * 8 < a.dim ? this->piece * 8 : 0;
+            const int64_t at = 2 * (((((int64_t)pages[c] * a.kv_heads + hk) << a.page_shift) + (j & ((1 << a.page_shift) - 1))) * a.dim + piece);
+            to_lds(a.k.p + at, lds_address(kt) + wave * 1024 + 4096 * c);
+            to_lds(a.v.p + at, lds_address(vt) + wave * 1024 + 4096 * c);
+        }
+    }
+};
+
+// Many rows: a work item is 128 rows of one group, the four waves share tiles of 64 keys, two in LDS in turn.  Bound by the matrix cores
+// and by what LDS delivers to them (one operand of each product comes from there).
 template <class T, int DP, bool E8> __global__ __launch_bounds__(NT, 2) void attend_many(AttendArgs a) {
     using Row = Rows32<T, DP>;
-    __shared__ __attribute__((aligned(16))) short tile[2][2][KT * DP];
+    constexpr int ROWS = 128;
+    __shared__ __attribute__((aligned(1024))) short tile[2][2][KT * DP];
     __shared__ uint64_t good_rows[2], odd_rows[2][4];
     const Item it = block_of(a, blockIdx.x);
     if (it.group >= a.groups) return;
     const int b = it.group / a.kv_heads, hk = it.group % a.kv_heads;
     const Sequence s = sequence_of(a, b);
-    const int rows = min(s.nq, a.max_q) * a.group, r0 = it.tile * 128;
+    const int rows = min(s.nq, a.max_q) * a.group, r0 = it.tile * ROWS;
     if (r0 >= rows) return;
     const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6);
 
-    const Limits first = limits_of(a, s, r0 / a.group), last = limits_of(a, s, min(r0 + 127, rows - 1) / a.group);
+    const Limits first = limits_of(a, s, r0 / a.group), last = limits_of(a, s, min(r0 + ROWS - 1, rows - 1) / a.group);
     const Tiles tiles = tiles_of<KT>(first, last, a.sinks);
     int n = it.part * a.chunk, end = tiles.count;
     if (a.parts > 1) end = min(end, n + a.chunk);
@@ -197,34 +224,67 @@ template <class T, int DP, bool E8> __global__ __launch_bounds__(NT, 2) void att
     const Limits wfirst = limits_of(a, s, min(w0, rows - 1) / a.group), wlast = limits_of(a, s, min(w0 + 31, rows - 1) / a.group);
     const bool idle = w0 >= rows;
     const float c = a.scale * LOG2E;
+    auto whole = [&](int key0) { return key0 + KT <= first.hi && (key0 >= last.lo || key0 + KT <= a.sinks); };
 
     Row r;
     r.start(a, a.q.p, (int64_t)(s.q0 + token) * a.q.row + (int64_t)head * a.q.head, lane);
+    auto step = [&](int buf, int key0, uint64_t ok, uint64_t odd) {
+        const bool none = idle || key0 >= wlast.hi || (key0 + KT <= wfirst.lo && key0 >= a.sinks);
+        const bool full = key0 + KT <= wfirst.hi && (key0 >= wlast.lo || key0 + KT <= a.sinks) && ok == ~0ull && odd == 0;
+        if (!none) r.template step<2>(tile[buf][0], tile[buf][1], key0, !full, ok, odd, mine, a.sinks, c, lane);
+    };
     if (n < end) {
-        Stage<T, DP, E8, KT, NT> next;
-        uint64_t good = 0;
-        auto fetch = [&](int t) {
-            next.load(a, s, b, hk, tiles[t] * KT, tid);
-            if (wave == 0) good = good_pages(a, s, b, tiles[t] * KT, lane);
-        };
-        auto keep = [&](int t, int buf) {
-            const int key0 = tiles[t] * KT;
-            const uint64_t odd = next.store(tile[buf][0], tile[buf][1], tid, !(key0 + KT <= first.hi && (key0 >= last.lo || key0 + KT <= a.sinks)));
-            if (lane == 0) odd_rows[buf][wave] = odd;
-            if (tid == 0) good_rows[buf] = good;
-        };
-        fetch(n);
-        keep(n, n & 1);
-        __syncthreads();
-        for (; n < end; ++n) {
-            const int buf = n & 1, key0 = tiles[n] * KT;
-            if (n + 1 < end) fetch(n + 1);
-            const uint64_t ok = good_rows[buf], odd = odd_rows[buf][0] | odd_rows[buf][1] | odd_rows[buf][2] | odd_rows[buf][3];
-            const bool none = idle || key0 >= wlast.hi || (key0 + KT <= wfirst.lo && key0 >= a.sinks);
-            const bool full = key0 + KT <= wfirst.hi && (key0 >= wlast.lo || key0 + KT <= a.sinks) && ok == ~0ull && odd == 0;
-            if (!none) r.template step<2>(tile[buf][0], tile[buf][1], key0, !full, ok, odd, mine, a.sinks, c, lane);
-            if (n + 1 < end) keep(n + 1, buf ^ 1);
+        if constexpr (E8) {
+            Stage<T, DP, E8, KT, NT> next;
+            uint64_t good = 0;
+            auto fetch = [&](int t) {
+                next.load(a, s, b, hk, tiles[t] * KT, tid);
+                if (wave == 0) good = good_pages(a, s, b, tiles[t] * KT, lane);
+            };
+            auto keep = [&](int t, int buf) {
+                const uint64_t odd = next.store(tile[buf][0], tile[buf][1], tid, !whole(tiles[t] * KT));
+                if (lane == 0) odd_rows[buf][wave] = odd;
+                if (tid == 0) good_rows[buf] = good;
+            };
+            fetch(n);
+            keep(n, n & 1);
             __syncthreads();
+            for (; n < end; ++n) {
+                const int buf = n & 1;
+                if (n + 1 < end) fetch(n + 1);
+                step(buf, tiles[n] * KT, good_rows[buf], odd_rows[buf][0] | odd_rows[buf][1] | odd_rows[buf][2] | odd_rows[buf][3]);
+                if (n + 1 < end) keep(n + 1, buf ^ 1);
+                __syncthreads();
+            }
+        } else {
+            Direct<T, DP> src;
+            src.start(a, s, hk, wave, lane);
+            uint64_t ok = 0, next_ok = 0;
+            auto fetch = [&](int t, int buf) {             // its pages are looked up; those of the tile after it follow
+                src.issue(a, s, hk, tiles[t] * KT, tile[buf][0], tile[buf][1], wave);
+                next_ok = good_pages(a, s, b, tiles[t] * KT, lane);
+                if (t + 1 < end) src.look(a, s, b, tiles[t + 1] * KT);
+            };
+            // waits for the loads of tile t; cleans it where the mask cuts it for the block
+            auto take = [&](int t, int buf) -> uint64_t {
+                arrived();
+                __syncthreads();
+                ok = next_ok;
+                if (whole(tiles[t] * KT) && ok == ~0ull) return 0;
+                const uint64_t odd = clean_tile<T, DP, KT>(tile[buf][1], tid);
+                if (lane == 0) odd_rows[buf][wave] = odd;
+                __syncthreads();
+                return odd_rows[buf][0] | odd_rows[buf][1] | odd_rows[buf][2] | odd_rows[buf][3];
+            };
+            src.look(a, s, b, tiles[n] * KT);
+            fetch(n, n & 1);
+            uint64_t odd = take(n, n & 1);
+            for (; n < end; ++n) {
+                const int buf = n & 1;
+                if (n + 1 < end) fetch(n + 1, buf ^ 1);
+                step(buf, tiles[n] * KT, ok, odd);
+                if (n + 1 < end) odd = take(n + 1, buf ^ 1);
+            }
         }
     }
     const float all = both_halves_sum(r.l), by = both_halves_sum(r.spoil) + (all > 0.f ? 1.f / all : all == all ? 0.f : all);

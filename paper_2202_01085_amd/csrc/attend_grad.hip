@@ -16,7 +16,7 @@ namespace {
 
 constexpr int NT = 256;
 
-// stat = (log2 of the row's sum, or +inf for an empty row, so that its weights are 0; dO.O): 16 lanes to a row, 8 values each
+// stat: log2 of the row's sum, or +inf for an empty row, so that its weights are 0, and dO.O; 16 lanes to a row, 8 values each
 template <class T> __global__ __launch_bounds__(NT) void row_stats(AttendArgs a) {
     const int64_t row = (int64_t)blockIdx.x * 16 + threadIdx.x / 16, all = a.total_q * a.heads;
     const int x = threadIdx.x % 16 * 8;
@@ -35,7 +35,8 @@ template <class T> __global__ __launch_bounds__(NT) void row_stats(AttendArgs a)
         const float l = a.lse[row];
         const bool empty = l == NO_KEY;
         // a row whose dO or O is not finite makes what it adds to its keys NaN (also where tiles are cleaned)
-        a.stat[row] = make_float2(empty ? __builtin_inff() : l * LOG2E + (sum - sum), empty ? 0.f : sum);
+        a.stat[head * a.total_q + token] = empty ? __builtin_inff() : l * LOG2E + (sum - sum);
+        a.stat[(a.heads + head) * a.total_q + token] = empty ? 0.f : sum;
     }
 }
 
@@ -65,43 +66,10 @@ struct Unit {
 };
 constexpr float LEAST_UNIT = 0x1p-100f;
 
-// a tile of N rows of DP values from two tensors, on its way from memory to LDS
-template <class T, int DP, int N> struct Pair {
-    static constexpr int PIECES = DP / 8, COUNT = (N * PIECES + NT - 1) / NT;
-    static constexpr bool ALL = N * PIECES % NT == 0;
-    u32x4 x[COUNT], y[COUNT];
-    template <class At> __device__ void load(const Rows &p, const Rows &q, int dim, int tid, At &&at) {   // at(row): (row of the tensors, head)
-#pragma unroll
-        for (int c = 0; c < COUNT; ++c) {
-            const int i = tid + NT * c, row = i / PIECES, piece = i % PIECES;
-            if (!ALL && row >= N) break;
-            const int2 w = at(row);
-            x[c] = load_piece<DP>(p.p, (int64_t)w.x * p.row + (int64_t)w.y * p.head, piece, dim);
-            y[c] = load_piece<DP>(q.p, (int64_t)w.x * q.row + (int64_t)w.y * q.head, piece, dim);
-        }
-    }
-    __device__ void clean(bool second) {
-#pragma unroll
-        for (int c = 0; c < COUNT; ++c) {
-            x[c] = cleaned<T>(x[c]);
-            if (second) y[c] = cleaned<T>(y[c]);
-        }
-    }
-    __device__ void store(short *tx, short *ty, int tid) const {
-#pragma unroll
-        for (int c = 0; c < COUNT; ++c) {
-            const int i = tid + NT * c, row = i / PIECES, piece = i % PIECES;
-            if (!ALL && row >= N) break;
-            *(u32x4 *)(tx + tile_at<DP>(row, piece)) = x[c];
-            *(u32x4 *)(ty + tile_at<DP>(row, piece)) = y[c];
-        }
-    }
-};
-
 // dQ: 128 rows of one group to a block, 32 to a wave, tiles of 64 keys through LDS, as the forward kernel
 template <class T, int DP> __global__ __launch_bounds__(NT, 2) void grad_rows(AttendArgs a) {
     constexpr int KS = DP / 16, DB = DP / 32, KT = 64;
-    __shared__ __attribute__((aligned(16))) short tile[2][2][KT * DP];
+    __shared__ __attribute__((aligned(1024))) short tile[2][2][KT * DP];
     const Item it = block_of(a, blockIdx.x);
     if (it.group >= a.groups) return;
     const int b = it.group / a.kv_heads, hk = it.group % a.kv_heads;
@@ -117,7 +85,7 @@ template <class T, int DP> __global__ __launch_bounds__(NT, 2) void grad_rows(At
     const Limits mine = limits_of(a, s, token);
     const Limits wfirst = limits_of(a, s, min(w0, rows - 1) / a.group), wlast = limits_of(a, s, min(w0 + 31, rows - 1) / a.group);
     const float c = a.scale * LOG2E;
-    const float2 stat = a.stat[(int64_t)(s.q0 + token) * a.heads + head];
+    const float lse2 = a.stat[(int64_t)head * a.total_q + s.q0 + token], delta = a.stat[(int64_t)(a.heads + head) * a.total_q + s.q0 + token];
 
     s16x8 q[KS], g[KS];
     f32x16 acc[DB];
@@ -138,10 +106,11 @@ template <class T, int DP> __global__ __launch_bounds__(NT, 2) void grad_rows(At
             d = T::mma(frag_r<DP>(vt, 32 * kb, ks, lane), g[ks], d);
         }
 #pragma unroll
-        for (int i = 0; i < 16; ++i) d[i] = __builtin_amdgcn_exp2f(__builtin_fmaf(p[i], c, -stat.x)) * (d[i] - stat.y);
+        for (int i = 0; i < 16; ++i) d[i] = __builtin_amdgcn_exp2f(__builtin_fmaf(p[i], c, -lse2)) * (d[i] - delta);
         if (edge) {
+            const uint32_t bits = (uint32_t)seen_bits(mine, a.sinks, key0 + 32 * kb) >> (4 * (lane >> 5));
 #pragma unroll
-            for (int i = 0; i < 16; ++i) d[i] = sees(mine, a.sinks, key0 + 32 * kb + c_row(i, lane)) ? d[i] : 0.f;
+            for (int i = 0; i < 16; ++i) d[i] = pick(bits, c_row(i, 0), d[i], 0.f);
         }
         unit.fit<T, DB>(d, acc);
 #pragma unroll
@@ -153,71 +122,91 @@ template <class T, int DP> __global__ __launch_bounds__(NT, 2) void grad_rows(At
     };
 
     if (tiles.count > 0) {
-        Pair<T, DP, KT> next;
-        // k is cleaned in tiles that the mask cuts for some row of the block: rows that see an infinity or NaN of k have such an lse
-        auto whole = [&](int key0) { return key0 + KT <= first.hi && (key0 >= last.lo || key0 + KT <= a.sinks); };
-        auto fetch = [&](int t) {
+        Tile2<T, DP, KT> src;
+        src.start(a.k.p + 2 * ((int64_t)s.k0 * a.k.row + (int64_t)hk * a.k.head), a.k.row, a.v.p + 2 * ((int64_t)s.k0 * a.v.row + (int64_t)hk * a.v.head), a.v.row, a.dim, wave, lane);
+        auto fetch = [&](int t, int buf) { src.issue(tiles[t] * KT, s.nk, a.dim, tile[buf][0], tile[buf][1], wave); };
+        // waits for the loads of tile t; k is cleaned where the mask cuts the tile for the block: rows that see an odd k have such an lse
+        auto take = [&](int t, int buf) {
+            arrived();
+            __syncthreads();
             const int key0 = tiles[t] * KT;
-            next.load(a.k, a.v, a.dim, tid, [&](int r) { return make_int2(s.k0 + min(key0 + r, s.nk - 1), hk); });
+            if (key0 + KT <= first.hi && (key0 >= last.lo || key0 + KT <= a.sinks)) return;
+            clean_tile<T, DP, KT>(tile[buf][0], tid);
+            __syncthreads();
         };
-        auto keep = [&](int t, int buf) {
-            if (!whole(tiles[t] * KT)) next.clean(false);
-            next.store(tile[buf][0], tile[buf][1], tid);
-        };
-        fetch(0);
-        keep(0, 0);
-        __syncthreads();
+        fetch(0, 0);
+        take(0, 0);
         for (int n = 0; n < tiles.count; ++n) {
             const int buf = n & 1, key0 = tiles[n] * KT;
-            if (n + 1 < tiles.count) fetch(n + 1);
+            if (n + 1 < tiles.count) fetch(n + 1, buf ^ 1);
             const bool none = idle || key0 >= wlast.hi || (key0 + KT <= wfirst.lo && key0 >= a.sinks);
             const bool full = key0 + KT <= wfirst.hi && (key0 >= wlast.lo || key0 + KT <= a.sinks);
             if (!none) {
                 block(tile[buf][0], tile[buf][1], 0, key0, !full);
                 block(tile[buf][0], tile[buf][1], 1, key0, !full);
             }
-            if (n + 1 < tiles.count) keep(n + 1, buf ^ 1);
-            __syncthreads();
+            if (n + 1 < tiles.count) take(n + 1, buf ^ 1);
         }
     }
     const float by = T::narrow ? a.scale * unit.u : a.scale;
     store_rows<T, DB>(acc, by, a.dq.p, (int64_t)(s.q0 + token) * a.dq.row + (int64_t)head * a.dq.head, a.dim, valid, lane);
 }
 
-// dK, dV: 128 keys of one group to a block, 32 to a wave with their k and v in registers; tiles of 32 rows of q and dO through LDS
+// A block of grad_keys: 128 keys of a group and the row tiles that see them, 32 tokens of one head each, head by head
+constexpr int RT = 32;
+struct KeyTile {
+    int lo, per_head, count;    // first token, row tiles of a head, of all heads of the group
+    int hi;                     // tokens [lo, hi)
+};
+// tokens that see keys of [from, to) are one interval: keys of the sinks stay visible to all later tokens
+__device__ __forceinline__ KeyTile key_tile(const AttendArgs &a, const Sequence &s, int from, int to) {
+    const int off = s.nk - s.nq, nq = min(s.nq, a.max_q);
+    KeyTile t;
+    t.lo = 0;
+    t.hi = nq;
+    if (a.causal) {
+        t.lo = min(max(from - off, 0), nq);
+        if (a.window && from >= a.sinks) t.hi = max(t.lo, (int)min((int64_t)nq, (int64_t)to - 1 + a.window - off));
+    }
+    t.per_head = (t.hi - t.lo + RT - 1) / RT;
+    t.count = t.per_head * a.group;
+    return t;
+}
+
+// dK, dV: 32 keys to a wave with their k and v in registers; tiles of q and dO through LDS, three in turn.  The scores of a tile are made
+// while the products of the one before it go into dV and dK: two independent streams of matrix instructions, and the exponentials
+// of one run under those of the other.
 template <class T, int DP> __global__ __launch_bounds__(NT, DP == 128 ? 1 : 2) void grad_keys(AttendArgs a) {
-    constexpr int KS = DP / 16, DB = DP / 32, RT = 32;
+    constexpr int KS = DP / 16, DB = DP / 32;
     constexpr float LIFT = T::narrow ? 12.f : 0.f;
-    __shared__ __attribute__((aligned(16))) short tile[2][2][RT * DP];
-    __shared__ __attribute__((aligned(16))) float lse2[2][RT], delta[2][RT];
-    __shared__ __attribute__((aligned(16))) int pos[2][RT];
+    __shared__ __attribute__((aligned(1024))) short tile[3][2][RT * DP];
+    __shared__ __attribute__((aligned(256))) float stat[3][2][RT];
     const Item it = block_of(a, blockIdx.x);
     if (it.group >= a.groups) return;
     const int b = it.group / a.kv_heads, hk = it.group % a.kv_heads;
     const Sequence s = sequence_of(a, b);
-    const int k0 = (a.tiles - 1 - it.tile) * 128;   // the first keys have most rows
+    const int at_tile = a.tiles - 1 - it.tile, k0 = at_tile * 128;   // the first keys have most rows
     if (k0 >= s.nk) return;
     const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6);
-    const int off = s.nk - s.nq, nq = min(s.nq, a.max_q);   // position of token 0
-
-    // tokens that see keys of [from, to): one interval, as keys of the sinks stay visible to all later tokens
-    auto tokens = [&](int from, int to) {
-        int lo = 0, hi = nq;
-        if (a.causal) {
-            lo = min(max(from - off, 0), nq);
-            if (a.window && from >= a.sinks) hi = max(lo, (int)min((int64_t)nq, (int64_t)to - 1 + a.window - off));
-        }
-        return make_int2(lo, hi);
-    };
-    const int2 span = tokens(k0, min(k0 + 128, s.nk));
-    const int row0 = span.x * a.group, row1 = span.y * a.group;
+    const int off = s.nk - s.nq;                                     // position of token 0
+    const KeyTile t = key_tile(a, s, k0, min(k0 + 128, s.nk));
+    const bool cut = at_tile < a.split && t.count > a.chunk;
+    if (!cut && it.part > 0) return;
+    int n = cut ? it.part * a.chunk : 0;
+    const int end = cut ? min(t.count, n + a.chunk) : t.count;
+    if (cut && n >= end) return;
 
     const int w0 = k0 + 32 * wave, key = w0 + (lane & 31), kept = min(key, s.nk - 1);
     const bool valid = key < s.nk, idle = w0 >= s.nk;
-    // positions [plo, phi) see this lane's key
-    const int plo = a.causal ? key : INT32_MIN;
-    const int64_t phi = !valid ? INT64_MIN : a.causal && a.window && key >= a.sinks ? (int64_t)key + a.window : INT64_MAX;
-    const int wl = min(w0 + 31, s.nk - 1);
+    // tokens [from, to) see this lane's key
+    const int from = !valid ? t.hi : a.causal ? max(key - off, 0) : 0;
+    const int to = a.causal && a.window && key >= a.sinks ? (int)min((int64_t)t.hi, (int64_t)key + a.window - off) : t.hi;
+    const KeyTile mine = key_tile(a, s, w0, min(w0 + 32, s.nk));     // of the wave: it has nothing to do elsewhere
+    // tokens [all0, all1) see all keys from x to y - 1
+    auto seen_by_all = [&](int x, int y, int t0) {
+        return y <= s.nk && t0 + RT <= t.hi &&
+               (!a.causal || (t0 >= y - 1 - off && (!a.window || t0 + RT - 1 + off < (int64_t)x + a.window || y <= a.sinks)));
+    };
     const float c = a.scale * LOG2E;
 
     s16x8 k[KS], v[KS];
@@ -231,91 +220,160 @@ template <class T, int DP> __global__ __launch_bounds__(NT, DP == 128 ? 1 : 2) v
     for (int db = 0; db < DB; ++db) { dk[db] = (f32x16)0.f; dv[db] = (f32x16)0.f; }
     Unit unit{LEAST_UNIT};
 
-    auto block = [&](int buf, int left, bool edge) {   // `left` rows of the tile exist
-        const short *qt = tile[buf][0], *gt = tile[buf][1];
-        f32x16 p = (f32x16)0.f, d = (f32x16)0.f;
-#pragma unroll
-        for (int ks = 0; ks < KS; ++ks) {
-            p = T::mma(frag_r<DP>(qt, 0, ks, lane), k[ks], p);
-            d = T::mma(frag_r<DP>(gt, 0, ks, lane), v[ks], d);
-        }
-#pragma unroll
-        for (int i4 = 0; i4 < 4; ++i4) {
-            const int r = c_row(4 * i4, lane);
-            const float4 l = *(const float4 *)&lse2[buf][r], e = *(const float4 *)&delta[buf][r];
-            const float ls[4] = {l.x, l.y, l.z, l.w}, de[4] = {e.x, e.y, e.z, e.w};
-#pragma unroll
-            for (int j = 0; j < 4; ++j) {
-                const int i = 4 * i4 + j;
-                p[i] = __builtin_amdgcn_exp2f(__builtin_fmaf(p[i], c, LIFT - ls[j]));
-                d[i] = p[i] * (d[i] - de[j]);
-            }
-        }
-        if (edge) {
-#pragma unroll
-            for (int i = 0; i < 16; ++i) {
-                const int r = c_row(i, lane), at = pos[buf][r];
-                const bool ok = r < left && at >= plo && at < phi;
-                p[i] = ok ? p[i] : 0.f;
-                d[i] = ok ? d[i] : 0.f;
-            }
-        }
-        unit.fit<T, DB>(d, dk);
-#pragma unroll
-        for (int h = 0; h < 2; ++h) {
-            const s16x8 w = as_operand<T>(p, h), u = as_operand<T>(d, h);
-#pragma unroll
-            for (int db = 0; db < DB; ++db) {
-                dv[db] = T::mma(frag_t<DP>(gt, 16 * h, db, lane), w, dv[db]);
-                dk[db] = T::mma(frag_t<DP>(qt, 16 * h, db, lane), u, dk[db]);
-            }
-        }
+    Tile2<T, DP, RT> src;
+    src.start(a.q.p + 2 * ((int64_t)s.q0 * a.q.row + (int64_t)hk * a.group * a.q.head), a.q.row, a.dout.p + 2 * ((int64_t)s.q0 * a.dout.row + (int64_t)hk * a.group * a.dout.head), a.dout.row,
+              a.dim, wave, lane);
+    const char *const q_base = src.base[0], *const g_base = src.base[1];
+    const float *const stats = a.stat + ((int64_t)(lane < 32 ? 0 : a.heads) + hk * a.group) * a.total_q + s.q0;
+    // tile n is tokens t0 .. t0 + 31 of head h
+    auto token_of = [&](int x) { return t.lo + x % t.per_head * RT; };
+    auto fetch = [&](int x, int buf) {
+        const int h = x / t.per_head, t0 = token_of(x);
+        src.base[0] = q_base + 2 * h * a.q.head;
+        src.base[1] = g_base + 2 * h * a.dout.head;
+        src.issue(t0, t.hi, a.dim, tile[buf][0], tile[buf][1], wave);
+        if (wave == 0) word_to_lds(stats + (int64_t)h * a.total_q + min(t0 + (lane & 31), t.hi - 1), lds_address((const short *)stat[buf]));
+    };
+    // waits for the loads of a tile; q and dO are cleaned where the mask cuts it for the block (rows with an odd value have such a stat)
+    auto take = [&](int x, int buf) {
+        arrived();
+        __syncthreads();
+        if (seen_by_all(k0, k0 + 128, token_of(x))) return;
+        clean_tile<T, DP, RT>(tile[buf][0], tid);
+        clean_tile<T, DP, RT>(tile[buf][1], tid);
+        __syncthreads();
     };
 
-    if (row0 < row1) {
-        Pair<T, DP, RT> next;
-        float2 st = make_float2(0.f, 0.f);
-        int at = 0;
-        auto fetch = [&](int r0) {
-            next.load(a.q, a.dout, a.dim, tid, [&](int r) {
-                const int x = min(r0 + r, row1 - 1);
-                return make_int2(s.q0 + x / a.group, hk * a.group + x % a.group);
-            });
-            if (tid < RT) {
-                const int x = min(r0 + tid, row1 - 1);
-                st = a.stat[(int64_t)(s.q0 + x / a.group) * a.heads + hk * a.group + x % a.group];
-                at = x / a.group + off;
+    s16x8 pw[2], dw[2];        // P and dS of the tile before, as operands
+    bool held = false;
+    auto add = [&](int buf) {
+#pragma unroll
+        for (int h = 0; h < 2; ++h)
+#pragma unroll
+            for (int db = 0; db < DB; ++db) {
+                dv[db] = T::mma(frag_t<DP>(tile[buf][1], 16 * h, db, lane), pw[h], dv[db]);
+                dk[db] = T::mma(frag_t<DP>(tile[buf][0], 16 * h, db, lane), dw[h], dk[db]);
             }
-        };
-        // positions of a tile's first and last row; q and dO are cleaned in tiles that the mask cuts for some key of the block (rows with
-        // an infinity or NaN have such a stat)
-        auto place = [&](int r0) { return make_int2(r0 / a.group + off, min(r0 + RT - 1, row1 - 1) / a.group + off); };
-        auto seen_by_all = [&](int2 at, int64_t from, int64_t to) {
-            return !a.causal || (at.x >= to - 1 && (!a.window || at.y < from + a.window || to <= a.sinks));
-        };
-        auto keep = [&](int r0, int buf) {
-            if (!(k0 + 128 <= s.nk && r0 + RT <= row1 && seen_by_all(place(r0), k0, k0 + 128))) next.clean(true);
-            next.store(tile[buf][0], tile[buf][1], tid);
-            if (tid < RT) { lse2[buf][tid] = st.x; delta[buf][tid] = st.y; pos[buf][tid] = at; }
-        };
-        fetch(row0);
-        keep(row0, 0);
-        __syncthreads();
-        int buf = 0;
-        for (int r0 = row0; r0 < row1; r0 += RT, buf ^= 1) {
-            if (r0 + RT < row1) fetch(r0 + RT);
-            const int2 at = place(r0);
-            const bool none = idle || (a.causal && (at.y < w0 || (a.window && w0 >= a.sinks && at.x >= (int64_t)wl + a.window)));
-            const bool full = w0 + 32 <= s.nk && r0 + RT <= row1 && seen_by_all(at, w0, w0 + 32);
-            if (!none) block(buf, row1 - r0, !full);
-            if (r0 + RT < row1) keep(r0 + RT, buf ^ 1);
-            __syncthreads();
+    };
+    if (n < end) {
+        fetch(n, 0);
+        take(n, 0);
+        int buf = 0, before = 2;
+        for (; n < end; ++n) {
+            const int next = before == 2 ? (buf == 0 ? 1 : 0) : 3 - buf - before;
+            if (n + 1 < end) fetch(n + 1, next);
+            const int t0 = token_of(n);
+            if (!idle && t0 < mine.hi && t0 + RT > mine.lo) {
+                const bool edge = !seen_by_all(w0, w0 + 32, t0);
+                f32x16 p = (f32x16)0.f, d = (f32x16)0.f;
+#pragma unroll
+                for (int ks = 0; ks < KS; ++ks) {
+                    p = T::mma(frag_r<DP>(tile[buf][0], 0, ks, lane), k[ks], p);
+                    d = T::mma(frag_r<DP>(tile[buf][1], 0, ks, lane), v[ks], d);
+                }
+                if (held) add(before);
+#pragma unroll
+                for (int i4 = 0; i4 < 4; ++i4) {
+                    const int r = c_row(4 * i4, lane);
+                    const float4 l = *(const float4 *)&stat[buf][0][r], e = *(const float4 *)&stat[buf][1][r];
+                    const float ls[4] = {l.x, l.y, l.z, l.w}, de[4] = {e.x, e.y, e.z, e.w};
+#pragma unroll
+                    for (int j = 0; j < 4; ++j) {
+                        const int i = 4 * i4 + j;
+                        p[i] = __builtin_amdgcn_exp2f(__builtin_fmaf(p[i], c, LIFT - ls[j]));
+                        d[i] = p[i] * (d[i] - de[j]);
+                    }
+                }
+                if (edge) {
+                    const uint32_t bits = (uint32_t)(below(to - t0) & ~below(from - t0)) >> (4 * (lane >> 5));
+#pragma unroll
+                    for (int i = 0; i < 16; ++i) {
+                        p[i] = pick(bits, c_row(i, 0), p[i], 0.f);
+                        d[i] = pick(bits, c_row(i, 0), d[i], 0.f);
+                    }
+                }
+                unit.fit<T, DB>(d, dk);
+#pragma unroll
+                for (int h = 0; h < 2; ++h) {
+                    pw[h] = as_operand<T>(p, h);
+                    dw[h] = as_operand<T>(d, h);
+                }
+                held = true;
+            } else if (held) {
+                add(before);
+                held = false;
+            }
+            if (n + 1 < end) take(n + 1, next);
+            before = buf;
+            buf = next;
         }
+        if (held) add(before);
     }
-    const int64_t to = s.k0 + kept;
-    store_rows<T, DB>(dv, T::narrow ? 0x1p-12f : 1.f, a.dv.p, to * a.dv.row + (int64_t)hk * a.dv.head, a.dim, valid, lane);
-    store_rows<T, DB>(dk, T::narrow ? a.scale * 0x1p-12f * unit.u : a.scale, a.dk.p, to * a.dk.row + (int64_t)hk * a.dk.head, a.dim, valid, lane);
+    const int64_t row = s.k0 + kept;
+    const float v_by = T::narrow ? 0x1p-12f : 1.f, k_by = T::narrow ? a.scale * 0x1p-12f * unit.u : a.scale;
+    if (cut) {     // fp32 sums of this part, for join_keys
+        float *to_part = a.part_out + ((((int64_t)it.group * a.split + at_tile) * a.parts + it.part) * 256 + 32 * wave + (lane & 31)) * a.dim;
+#pragma unroll
+        for (int db = 0; db < DB; ++db)
+#pragma unroll
+            for (int i = 0; i < 16; i += 4) {
+                const int x = 32 * db + c_row(i, lane);
+                if (x >= a.dim) continue;
+                *(float4 *)(to_part + x) = make_float4(dk[db][i] * k_by, dk[db][i + 1] * k_by, dk[db][i + 2] * k_by, dk[db][i + 3] * k_by);
+                *(float4 *)(to_part + (int64_t)128 * a.dim + x) = make_float4(dv[db][i] * v_by, dv[db][i + 1] * v_by, dv[db][i + 2] * v_by, dv[db][i + 3] * v_by);
+            }
+        return;
+    }
+    store_rows<T, DB>(dv, v_by, a.dv.p, row * a.dv.row + (int64_t)hk * a.dv.head, a.dim, valid, lane);
+    store_rows<T, DB>(dk, k_by, a.dk.p, row * a.dk.row + (int64_t)hk * a.dk.head, a.dim, valid, lane);
 }
+
+// the parts of the key tiles that were cut, summed in their order: a block to 8 keys of a tile, 32 lanes to a key, 4 values each
+template <class T> __global__ __launch_bounds__(NT) void join_keys(AttendArgs a) {
+    const int group = blockIdx.x / (16 * a.split), at_tile = blockIdx.x / 16 % a.split, k0 = at_tile * 128;
+    const int b = group / a.kv_heads, hk = group % a.kv_heads, in = blockIdx.x % 16 * 8 + threadIdx.x / 32, x = threadIdx.x % 32 * 4;
+    const Sequence s = sequence_of(a, b);
+    if (k0 + in >= s.nk || x >= a.dim) return;
+    const KeyTile t = key_tile(a, s, k0, min(k0 + 128, s.nk));
+    if (t.count <= a.chunk) return;
+    const int parts = (t.count + a.chunk - 1) / a.chunk;
+    const float *from = a.part_out + ((((int64_t)group * a.split + at_tile) * a.parts) * 256 + in) * a.dim + x;
+    float4 k = make_float4(0.f, 0.f, 0.f, 0.f), v = k;
+    for (int p = 0; p < parts; ++p, from += (int64_t)256 * a.dim) {
+        const float4 y = *(const float4 *)from, z = *(const float4 *)(from + (int64_t)128 * a.dim);
+        k.x += y.x; k.y += y.y; k.z += y.z; k.w += y.w;
+        v.x += z.x; v.y += z.y; v.z += z.z; v.w += z.w;
+    }
+    const int64_t row = s.k0 + k0 + in;
+    *(u32x2 *)(a.dk.p + 2 * (row * a.dk.row + (int64_t)hk * a.dk.head + x)) = (u32x2){T::pack(k.x, k.y), T::pack(k.z, k.w)};
+    *(u32x2 *)(a.dv.p + 2 * (row * a.dv.row + (int64_t)hk * a.dv.head + x)) = (u32x2){T::pack(v.x, v.y), T::pack(v.z, v.w)};
+}
+
+// How grad_keys is cut.  A block has a CU to itself at head sizes above 64, half of one below: 256 or 512 at a time.  With a window all key
+// tiles have about the same rows, but those of the sinks, which all later tokens see: these are cut to the others' size.  Without, the
+// tiles are cut where they are too few to even out their lengths.
+void cut_keys(AttendArgs &a, int64_t max_k) {
+    const int64_t tiles = cdiv(max_k, 128), items = tiles * a.groups, slots = a.dim > 64 ? 256 : 512;
+    const int64_t longest = cdiv(a.max_q, RT) * a.group, windowed = (cdiv((int64_t)a.window + 128, RT) + 1) * a.group;
+    a.tiles = (int)tiles;
+    a.split = 0;
+    a.parts = 1;
+    a.chunk = 0;
+    if (a.window && windowed < longest) {
+        a.split = (int)std::min(tiles, cdiv(a.sinks, 128));
+        a.chunk = (int)windowed;
+    } else if (items < 2 * slots) {
+        a.split = (int)tiles;
+        a.chunk = (int)std::max<int64_t>(8, cdiv(items * longest / (a.causal ? 2 : 1), slots));
+    }
+    if (a.split) a.parts = (int)cdiv(longest, a.chunk);
+    if (a.parts <= 1) {
+        a.parts = 1;
+        a.split = 0;
+    }
+}
+
+int64_t stat_floats(const AttendArgs &a) { return cdiv(2 * a.total_q * a.heads, 64) * 64; }
 
 template <class T, int DP> void launch(AttendArgs a, int64_t max_k, hipStream_t st) {
     if (a.max_q && a.total_q) {
@@ -327,20 +385,32 @@ template <class T, int DP> void launch(AttendArgs a, int64_t max_k, hipStream_t 
         F3M_HIP(hipGetLastError());
     }
     if (max_k && a.total_k) {
-        a.tiles = (int)cdiv(max_k, 128);
-        const int64_t blocks = attend_blocks(a, a.tiles);
+        cut_keys(a, max_k);
+        const int64_t blocks = attend_blocks(a, (int64_t)a.tiles * a.parts);
         grad_keys<T, DP><<<dim3((uint32_t)blocks), NT, 0, st>>>(a);
         F3M_HIP(hipGetLastError());
+        if (a.split) {
+            join_keys<T><<<dim3((uint32_t)((int64_t)a.groups * a.split * 16)), NT, 0, st>>>(a);
+            F3M_HIP(hipGetLastError());
+        }
     }
 }
 
 }  // namespace
 
-int64_t attend_grad_workspace(const AttendArgs &a) { return a.total_q * a.heads * (int64_t)sizeof(float2); }
+int64_t attend_grad_workspace(AttendArgs a, int64_t max_k) {
+    int64_t floats = stat_floats(a);
+    if (max_k && a.total_k) {
+        cut_keys(a, max_k);
+        floats += (int64_t)a.groups * a.split * (a.split ? a.parts : 0) * 256 * a.dim;
+    }
+    return floats * (int64_t)sizeof(float);
+}
 
 void run_attend_grad(AttendArgs a, int64_t max_k, bool f16, void *workspace, hipStream_t st) {
     if (!a.groups) return;
-    a.stat = (float2 *)workspace;
+    a.stat = (float *)workspace;
+    a.part_out = a.stat + stat_floats(a);
     a.parts = 1;
     if (a.dim <= 32) f16 ? launch<F16, 32>(a, max_k, st) : launch<Bf16, 32>(a, max_k, st);
     else if (a.dim <= 64) f16 ? launch<F16, 64>(a, max_k, st) : launch<Bf16, 64>(a, max_k, st);
