@@ -37,7 +37,7 @@ struct AttendArgs {
     float *part_out, *part_lse;               // (parts, rows of q, heads, dim) and (parts, rows of q, heads)
     // gradient
     Rows dout, dq, dk, dv;
-    float *stat;                              // (2, heads, rows of q): log2 of the row's sum (inf: empty row), dO.O
+    float *stat;                              // (2, heads, rows of q): -log2 of the row's sum (-inf: empty row), -dO.O
     int split;                                // key tiles of a group that may be cut into parts; chunk is in row tiles there
 };
 
@@ -263,11 +263,12 @@ __device__ __forceinline__ Place place_of(const AttendArgs &a, const Sequence &s
 // 16 bytes to a lane, 1 KB to an instruction, in the order of LDS: lane i's bytes go to `lds` + 16 i.  So which piece of which row a lane
 // reads follows from where it has to lie (tile_at).  Written out, because the compiler, which cannot tell the tiles apart, would wait
 // for the loads before every transposing read of another tile; nothing comes back in registers, and arrived() waits for them.
-__device__ __forceinline__ u32x4 buffer_of(const char *p, int64_t bytes) {   // reads past `bytes` give zeros
+__device__ __forceinline__ u32x4 buffer_of(const char *p, int bytes) {   // reads past `bytes` give zeros
     const uint64_t at = (uint64_t)p;
     return (u32x4){(uint32_t)__builtin_amdgcn_readfirstlane((uint32_t)at), (uint32_t)__builtin_amdgcn_readfirstlane((uint32_t)(at >> 32)),
-                   (uint32_t)__builtin_amdgcn_readfirstlane((uint32_t)min(max(bytes, (int64_t)0), (int64_t)0x7fffffff)), 0x00020000u};
+                   (uint32_t)__builtin_amdgcn_readfirstlane((uint32_t)bytes), 0x00020000u};
 }
+constexpr uint32_t NOWHERE = 0xffffff00u;   // an offset past every buffer
 __device__ __forceinline__ void to_lds(u32x4 buffer, uint32_t lane_offset, uint32_t offset, uint32_t lds) {
     asm volatile("s_mov_b32 m0, %0\n\tbuffer_load_dwordx4 %1, %2, %3 offen lds" ::"s"(__builtin_amdgcn_readfirstlane(lds)), "v"(lane_offset),
                  "s"(buffer), "s"(__builtin_amdgcn_readfirstlane(offset)) : "memory");
@@ -278,47 +279,51 @@ __device__ __forceinline__ void to_lds(const char *p, uint32_t lds) {
 __device__ __forceinline__ void word_to_lds(const float *p, uint32_t lds) {   // 4 bytes to a lane
     asm volatile("s_mov_b32 m0, %0\n\tglobal_load_lds_dword %1, off" ::"s"(__builtin_amdgcn_readfirstlane(lds)), "v"(p) : "memory");
 }
-__device__ __forceinline__ void arrived() { asm volatile("s_waitcnt vmcnt(0)" ::: "memory"); }
+// waits until at most LEFT of the wave's loads are under way (they arrive in the order of their issue)
+template <int LEFT = 0> __device__ __forceinline__ void arrived() { asm volatile("s_waitcnt vmcnt(%0)" ::"i"(LEFT) : "memory"); }
+// Waits for loads that came back in registers, where the compiler sees it: it would otherwise wait at their first use inside a loop, and
+// there for all loads under way, the next tiles' too
+__device__ __forceinline__ void registers_loaded() { __builtin_amdgcn_s_waitcnt(0x0f70); }   // vmcnt(0)
 using lds_short = __attribute__((address_space(3))) short;
 __device__ __forceinline__ uint32_t lds_address(const short *p) { return (uint32_t)(uintptr_t)(const lds_short *)p; }
 
-// Tiles of N rows from two tensors (keys and values, say) with fixed strides, for a block of four waves
-template <class T, int DP, int N> struct Tile2 {
-    static constexpr int PIECES = DP / 8, RPI = 64 / PIECES, STEP = 4 * RPI, COUNT = (N + STEP - 1) / STEP;   // rows to an instruction, of four waves
+// Tiles of N rows from two tensors (keys and values, say) with fixed strides, for a block of WAVES waves
+template <class T, int DP, int N, int WAVES = 4> struct Tile2 {
+    static constexpr int PIECES = DP / 8, RPI = 64 / PIECES, STEP = WAVES * RPI, COUNT = (N + STEP - 1) / STEP;   // rows to an instruction, of all waves
     uint32_t off[2];           // the lane's bytes within the wave's first instruction
     int row, piece;            // the lane's row there, its piece
     const char *base[2];       // row 0
-    int64_t stride[2];
+    int stride[2];             // bytes between rows, below 2^23
 
     __device__ void start(const char *x, int64_t xrow, const char *y, int64_t yrow, int dim, int wave, int lane) {
         row = wave * RPI + lane / PIECES;
         piece = (lane % PIECES) ^ piece_swap<DP>(row);
         base[0] = x;
         base[1] = y;
-        stride[0] = 2 * xrow;
-        stride[1] = 2 * yrow;
+        stride[0] = 2 * (int)xrow;
+        stride[1] = 2 * (int)yrow;
 #pragma unroll
         for (int w = 0; w < 2; ++w)                        // zeros where the tile is wider than the head
-            off[w] = piece * 8 >= dim ? 0x7fffff00u : (uint32_t)(row * (int)stride[w] + piece * 16);
+            off[w] = piece * 8 >= dim ? NOWHERE : (uint32_t)(row * stride[w] + piece * 16);
     }
     // rows from row0 on; rows from `end` on give zeros
     __device__ void issue(int row0, int end, int dim, const short *tx, const short *ty, int wave) const {
         if (N < STEP && wave * RPI >= N) return;
 #pragma unroll
         for (int w = 0; w < 2; ++w) {
-            const u32x4 buffer = buffer_of(base[w] + row0 * stride[w], (end - 1 - row0) * stride[w] + 2 * dim);
+            const u32x4 buffer = buffer_of(base[w] + (int64_t)row0 * stride[w], (min(end - row0, N) - 1) * stride[w] + 2 * dim);
             const uint32_t lds = lds_address(w ? ty : tx) + wave * 1024;
 #pragma unroll
-            for (int c = 0; c < COUNT; ++c) to_lds(buffer, off[w], (uint32_t)(STEP * c * (int)stride[w]), lds + 4096 * c);
+            for (int c = 0; c < COUNT; ++c) to_lds(buffer, off[w], (uint32_t)(STEP * c * stride[w]), lds + 1024 * WAVES * c);
         }
     }
 };
 // infinities and NaN of a tile become 0; bits of the rows that had one (a wave's)
-template <class T, int DP, int N> __device__ __forceinline__ uint64_t clean_tile(short *tile, int tid) {
+template <class T, int DP, int N, int THREADS = 256> __device__ __forceinline__ uint64_t clean_tile(short *tile, int tid) {
     constexpr int PIECES = DP / 8;
     uint64_t odd = 0;
 #pragma unroll
-    for (int at = tid; at < N * PIECES; at += 256) {
+    for (int at = tid; at < N * PIECES; at += THREADS) {
         const u32x4 w = *(const u32x4 *)(tile + 8 * at);
         if (any_odd<T>(w)) {
             *(u32x4 *)(tile + 8 * at) = cleaned<T>(w);

@@ -233,6 +233,7 @@ template <class T, int DP, bool E8> __global__ __launch_bounds__(NT, 2) void att
         const bool full = key0 + KT <= wfirst.hi && (key0 >= wlast.lo || key0 + KT <= a.sinks) && ok == ~0ull && odd == 0;
         if (!none) r.template step<2>(tile[buf][0], tile[buf][1], key0, !full, ok, odd, mine, a.sinks, c, lane);
     };
+    registers_loaded();
     if (n < end) {
         if constexpr (E8) {
             Stage<T, DP, E8, KT, NT> next;
@@ -337,6 +338,7 @@ template <class T, int DP, bool E8> __global__ __launch_bounds__(NT, 2) void att
 
     Row r;
     r.start(a, a.q.p, (int64_t)(s.q0 + token) * a.q.row + (int64_t)head * a.q.head, lane);
+    registers_loaded();
     short *kt = tile[wave][0], *vt = tile[wave][1];
     if (n < end) {
         Stage<T, DP, E8, N, 64> next;

@@ -16,7 +16,10 @@ namespace {
 
 constexpr int NT = 256;
 
-// stat: log2 of the row's sum, or +inf for an empty row, so that its weights are 0, and dO.O; 16 lanes to a row, 8 values each
+// log2 of the factor that grad_keys holds weights with
+template <class T> constexpr float LIFT = T::narrow ? 12.f : 0.f;
+
+// stat: -log2 of the row's sum (+ LIFT), or -inf for an empty row, so that its weights are 0, and -dO.O; 16 lanes to a row, 8 values each
 template <class T> __global__ __launch_bounds__(NT) void row_stats(AttendArgs a) {
     const int64_t row = (int64_t)blockIdx.x * 16 + threadIdx.x / 16, all = a.total_q * a.heads;
     const int x = threadIdx.x % 16 * 8;
@@ -35,8 +38,8 @@ template <class T> __global__ __launch_bounds__(NT) void row_stats(AttendArgs a)
         const float l = a.lse[row];
         const bool empty = l == NO_KEY;
         // a row whose dO or O is not finite makes what it adds to its keys NaN (also where tiles are cleaned)
-        a.stat[head * a.total_q + token] = empty ? __builtin_inff() : l * LOG2E + (sum - sum);
-        a.stat[(a.heads + head) * a.total_q + token] = empty ? 0.f : sum;
+        a.stat[head * a.total_q + token] = empty ? NO_KEY : LIFT<T> - l * LOG2E + (sum - sum);
+        a.stat[(a.heads + head) * a.total_q + token] = empty ? 0.f : -sum;
     }
 }
 
@@ -85,7 +88,7 @@ template <class T, int DP> __global__ __launch_bounds__(NT, 2) void grad_rows(At
     const Limits mine = limits_of(a, s, token);
     const Limits wfirst = limits_of(a, s, min(w0, rows - 1) / a.group), wlast = limits_of(a, s, min(w0 + 31, rows - 1) / a.group);
     const float c = a.scale * LOG2E;
-    const float lse2 = a.stat[(int64_t)head * a.total_q + s.q0 + token], delta = a.stat[(int64_t)(a.heads + head) * a.total_q + s.q0 + token];
+    const float less = a.stat[(int64_t)head * a.total_q + s.q0 + token] - LIFT<T>, delta = a.stat[(int64_t)(a.heads + head) * a.total_q + s.q0 + token];
 
     s16x8 q[KS], g[KS];
     f32x16 acc[DB];
@@ -99,14 +102,14 @@ template <class T, int DP> __global__ __launch_bounds__(NT, 2) void grad_rows(At
     Unit unit{LEAST_UNIT};
 
     auto block = [&](const short *kt, const short *vt, int kb, int key0, bool edge) {
-        f32x16 p = (f32x16)0.f, d = (f32x16)0.f;
+        f32x16 p = (f32x16)0.f, d = (f32x16)delta;     // dP starts from -dO.O
 #pragma unroll
         for (int ks = 0; ks < KS; ++ks) {
             p = T::mma(frag_r<DP>(kt, 32 * kb, ks, lane), q[ks], p);
             d = T::mma(frag_r<DP>(vt, 32 * kb, ks, lane), g[ks], d);
         }
 #pragma unroll
-        for (int i = 0; i < 16; ++i) d[i] = __builtin_amdgcn_exp2f(__builtin_fmaf(p[i], c, -lse2)) * (d[i] - delta);
+        for (int i = 0; i < 16; ++i) d[i] = __builtin_amdgcn_exp2f(__builtin_fmaf(p[i], c, less)) * d[i];
         if (edge) {
             const uint32_t bits = (uint32_t)seen_bits(mine, a.sinks, key0 + 32 * kb) >> (4 * (lane >> 5));
 #pragma unroll
@@ -121,6 +124,7 @@ template <class T, int DP> __global__ __launch_bounds__(NT, 2) void grad_rows(At
         }
     };
 
+    registers_loaded();
     if (tiles.count > 0) {
         Tile2<T, DP, KT> src;
         src.start(a.k.p + 2 * ((int64_t)s.k0 * a.k.row + (int64_t)hk * a.k.head), a.k.row, a.v.p + 2 * ((int64_t)s.k0 * a.v.row + (int64_t)hk * a.v.head), a.v.row, a.dim, wave, lane);
@@ -152,14 +156,14 @@ template <class T, int DP> __global__ __launch_bounds__(NT, 2) void grad_rows(At
     store_rows<T, DB>(acc, by, a.dq.p, (int64_t)(s.q0 + token) * a.dq.row + (int64_t)head * a.dq.head, a.dim, valid, lane);
 }
 
-// A block of grad_keys: 128 keys of a group and the row tiles that see them, 32 tokens of one head each, head by head
-constexpr int RT = 32;
+// A block of grad_keys: 128 keys of a group and the row tiles that see them, `rt` tokens of one head each: the heads of the group for
+// the first tokens, then for the next.  Blocks begin with different heads: rows of one head lie a multiple of its size apart, so that
+// blocks that all read the same head would all wait for a few channels of the caches.
 struct KeyTile {
-    int lo, per_head, count;    // first token, row tiles of a head, of all heads of the group
-    int hi;                     // tokens [lo, hi)
+    int lo, hi, count;    // tokens [lo, hi), row tiles of all heads
 };
 // tokens that see keys of [from, to) are one interval: keys of the sinks stay visible to all later tokens
-__device__ __forceinline__ KeyTile key_tile(const AttendArgs &a, const Sequence &s, int from, int to) {
+__device__ __forceinline__ KeyTile key_tile(const AttendArgs &a, const Sequence &s, int from, int to, int rt) {
     const int off = s.nk - s.nq, nq = min(s.nq, a.max_q);
     KeyTile t;
     t.lo = 0;
@@ -168,124 +172,141 @@ __device__ __forceinline__ KeyTile key_tile(const AttendArgs &a, const Sequence 
         t.lo = min(max(from - off, 0), nq);
         if (a.window && from >= a.sinks) t.hi = max(t.lo, (int)min((int64_t)nq, (int64_t)to - 1 + a.window - off));
     }
-    t.per_head = (t.hi - t.lo + RT - 1) / RT;
-    t.count = t.per_head * a.group;
+    t.count = (t.hi - t.lo + rt - 1) / rt * a.group;
     return t;
 }
 
-// dK, dV: 32 keys to a wave with their k and v in registers; tiles of q and dO through LDS, three in turn.  The scores of a tile are made
-// while the products of the one before it go into dV and dK: two independent streams of matrix instructions, and the exponentials
-// of one run under those of the other.
-template <class T, int DP> __global__ __launch_bounds__(NT, DP == 128 ? 1 : 2) void grad_keys(AttendArgs a) {
-    constexpr int KS = DP / 16, DB = DP / 32;
-    constexpr float LIFT = T::narrow ? 12.f : 0.f;
-    __shared__ __attribute__((aligned(1024))) short tile[3][2][RT * DP];
-    __shared__ __attribute__((aligned(256))) float stat[3][2][RT];
+// rows of a tile of grad_keys, by head size
+constexpr int rows_of_tile(int dp) { return dp == 128 ? 64 : 32; }
+
+// dK, dV: 32 keys to a wave, whose sums stay in registers; tiles of q and dO come through a ring in LDS, two or more under way while one
+// is worked on.  Head sizes above 64: the sums alone are 128 registers, so that two waves to a SIMD, which the exponentials of one
+// need to run under the products of the other, leave room for k only and v stays in LDS.  There a block has eight waves, two to the same
+// keys, each with every other 32 rows; their sums are added at the end.
+template <class T, int DP> __global__ __launch_bounds__(DP == 128 ? 512 : 256, 2) void grad_keys(AttendArgs a) {
+    constexpr int KS = DP / 16, DB = DP / 32, HALVES = DP == 128 ? 2 : 1, WAVES = 4 * HALVES, THREADS = 64 * WAVES, RT = rows_of_tile(DP);
+    constexpr bool V_LDS = DP == 128;
+    constexpr int AHEAD = DP == 128 ? 2 : 4, RING = AHEAD + 1, SLOT = 2 * RT * DP;
+    using Src = Tile2<T, DP, RT, WAVES>;
+    __shared__ __attribute__((aligned(1024))) short lds[RING * SLOT + (V_LDS ? 128 * DP : 0)];
+    __shared__ __attribute__((aligned(256))) float stat[RING][HALVES][WAVES][2][32];   // a copy to a wave, so that all waves have the same loads under way
+    short *const vt = lds + RING * SLOT;
     const Item it = block_of(a, blockIdx.x);
     if (it.group >= a.groups) return;
     const int b = it.group / a.kv_heads, hk = it.group % a.kv_heads;
     const Sequence s = sequence_of(a, b);
     const int at_tile = a.tiles - 1 - it.tile, k0 = at_tile * 128;   // the first keys have most rows
     if (k0 >= s.nk) return;
-    const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6);
+    const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6), kw = wave & 3, half = wave >> 2;
     const int off = s.nk - s.nq;                                     // position of token 0
-    const KeyTile t = key_tile(a, s, k0, min(k0 + 128, s.nk));
+    const KeyTile t = key_tile(a, s, k0, min(k0 + 128, s.nk), RT);
     const bool cut = at_tile < a.split && t.count > a.chunk;
     if (!cut && it.part > 0) return;
-    int n = cut ? it.part * a.chunk : 0;
-    const int end = cut ? min(t.count, n + a.chunk) : t.count;
-    if (cut && n >= end) return;
+    const int begin = cut ? it.part * a.chunk : 0, end = cut ? min(t.count, begin + a.chunk) : t.count;
+    if (cut && begin >= end) return;
 
-    const int w0 = k0 + 32 * wave, key = w0 + (lane & 31), kept = min(key, s.nk - 1);
+    const int w0 = k0 + 32 * kw, key = w0 + (lane & 31), kept = min(key, s.nk - 1);
     const bool valid = key < s.nk, idle = w0 >= s.nk;
     // tokens [from, to) see this lane's key
     const int from = !valid ? t.hi : a.causal ? max(key - off, 0) : 0;
     const int to = a.causal && a.window && key >= a.sinks ? (int)min((int64_t)t.hi, (int64_t)key + a.window - off) : t.hi;
-    const KeyTile mine = key_tile(a, s, w0, min(w0 + 32, s.nk));     // of the wave: it has nothing to do elsewhere
-    // tokens [all0, all1) see all keys from x to y - 1
-    auto seen_by_all = [&](int x, int y, int t0) {
-        return y <= s.nk && t0 + RT <= t.hi &&
-               (!a.causal || (t0 >= y - 1 - off && (!a.window || t0 + RT - 1 + off < (int64_t)x + a.window || y <= a.sinks)));
+    const KeyTile mine = key_tile(a, s, w0, min(w0 + 32, s.nk), RT);     // of the wave: it has nothing to do elsewhere
+    // tokens [all.x, all.y) see all keys x .. y - 1
+    auto seen_by_all = [&](int x, int y) {
+        if (y > s.nk) return make_int2(0, 0);
+        if (!a.causal) return make_int2(0, t.hi);
+        return make_int2(y - 1 - off, a.window && y > a.sinks ? (int)min((int64_t)t.hi, (int64_t)x + a.window - off) : t.hi);
     };
+    const int2 all_block = seen_by_all(k0, k0 + 128), all_wave = seen_by_all(w0, w0 + 32);
     const float c = a.scale * LOG2E;
 
-    s16x8 k[KS], v[KS];
+    s16x8 k[KS], v[V_LDS ? 1 : KS];
     f32x16 dk[DB], dv[DB];
 #pragma unroll
     for (int ks = 0; ks < KS; ++ks) {
         k[ks] = __builtin_bit_cast(s16x8, load_piece<DP>(a.k.p, (int64_t)(s.k0 + kept) * a.k.row + (int64_t)hk * a.k.head, 2 * ks + (lane >> 5), a.dim));
-        v[ks] = __builtin_bit_cast(s16x8, load_piece<DP>(a.v.p, (int64_t)(s.k0 + kept) * a.v.row + (int64_t)hk * a.v.head, 2 * ks + (lane >> 5), a.dim));
+        if (!V_LDS) v[V_LDS ? 0 : ks] = __builtin_bit_cast(s16x8, load_piece<DP>(a.v.p, (int64_t)(s.k0 + kept) * a.v.row + (int64_t)hk * a.v.head, 2 * ks + (lane >> 5), a.dim));
     }
+    if (V_LDS)
+        for (int at = tid; at < 128 * (DP / 8); at += THREADS) {
+            const int r = at / (DP / 8), piece = at % (DP / 8);
+            *(u32x4 *)(vt + tile_at<DP>(r, piece)) = load_piece<DP>(a.v.p, (int64_t)(s.k0 + min(k0 + r, s.nk - 1)) * a.v.row + (int64_t)hk * a.v.head, piece, a.dim);
+        }
 #pragma unroll
     for (int db = 0; db < DB; ++db) { dk[db] = (f32x16)0.f; dv[db] = (f32x16)0.f; }
     Unit unit{LEAST_UNIT};
 
-    Tile2<T, DP, RT> src;
-    src.start(a.q.p + 2 * ((int64_t)s.q0 * a.q.row + (int64_t)hk * a.group * a.q.head), a.q.row, a.dout.p + 2 * ((int64_t)s.q0 * a.dout.row + (int64_t)hk * a.group * a.dout.head), a.dout.row,
-              a.dim, wave, lane);
-    const char *const q_base = src.base[0], *const g_base = src.base[1];
+    // the next tile to load: tokens ft .. of head fh, the fn-th of the group for these tokens
+    Src src;
+    src.start(nullptr, a.q.row, nullptr, a.dout.row, a.dim, wave, lane);
+    int fn = begin % a.group, fh = (fn + at_tile) % a.group, ft = t.lo + begin / a.group * RT, fetched = begin;
+    const char *const q_base = a.q.p + 2 * ((int64_t)s.q0 * a.q.row + (int64_t)hk * a.group * a.q.head);
+    const char *const g_base = a.dout.p + 2 * ((int64_t)s.q0 * a.dout.row + (int64_t)hk * a.group * a.dout.head);
     const float *const stats = a.stat + ((int64_t)(lane < 32 ? 0 : a.heads) + hk * a.group) * a.total_q + s.q0;
-    // tile n is tokens t0 .. t0 + 31 of head h
-    auto token_of = [&](int x) { return t.lo + x % t.per_head * RT; };
-    auto fetch = [&](int x, int buf) {
-        const int h = x / t.per_head, t0 = token_of(x);
-        src.base[0] = q_base + 2 * h * a.q.head;
-        src.base[1] = g_base + 2 * h * a.dout.head;
-        src.issue(t0, t.hi, a.dim, tile[buf][0], tile[buf][1], wave);
-        if (wave == 0) word_to_lds(stats + (int64_t)h * a.total_q + min(t0 + (lane & 31), t.hi - 1), lds_address((const short *)stat[buf]));
+    // past the end the last tile is loaded again, which keeps the count of loads under way
+    auto fetch = [&](int slot) {
+        src.base[0] = q_base + 2 * fh * a.q.head;
+        src.base[1] = g_base + 2 * fh * a.dout.head;
+        src.issue(ft, t.hi, a.dim, lds + slot * SLOT, lds + slot * SLOT + RT * DP, wave);
+#pragma unroll
+        for (int h = 0; h < HALVES; ++h)
+            word_to_lds(stats + (int64_t)fh * a.total_q + min(ft + 32 * h + (lane & 31), t.hi - 1), lds_address((const short *)stat[slot][h][wave]));
+        if (++fetched < end) {
+            fh = fh + 1 < a.group ? fh + 1 : 0;
+            if (++fn == a.group) {
+                fn = 0;
+                ft += RT;
+            }
+        }
     };
-    // waits for the loads of a tile; q and dO are cleaned where the mask cuts it for the block (rows with an odd value have such a stat)
-    auto take = [&](int x, int buf) {
-        arrived();
+    constexpr int LOADS = 2 * Src::COUNT + HALVES;    // of a wave to a tile; HALVES of a wave that a small tile leaves nothing to
+    // waits for the loads of a tile, the AHEAD - 1 tiles after it stay under way; q and dO are cleaned where the mask cuts it for the block
+    // (rows with an odd value have such a stat)
+    auto take = [&](int t0, int slot) {
+        if (Src::STEP > RT && wave * Src::RPI >= RT) arrived<(AHEAD - 1) * HALVES>();
+        else arrived<(AHEAD - 1) * LOADS>();
         __syncthreads();
-        if (seen_by_all(k0, k0 + 128, token_of(x))) return;
-        clean_tile<T, DP, RT>(tile[buf][0], tid);
-        clean_tile<T, DP, RT>(tile[buf][1], tid);
+        if (t0 >= all_block.x && t0 + RT <= all_block.y) return;
+        clean_tile<T, DP, RT, THREADS>(lds + slot * SLOT, tid);
+        clean_tile<T, DP, RT, THREADS>(lds + slot * SLOT + RT * DP, tid);
         __syncthreads();
     };
 
-    s16x8 pw[2], dw[2];        // P and dS of the tile before, as operands
-    bool held = false;
-    auto add = [&](int buf) {
-#pragma unroll
-        for (int h = 0; h < 2; ++h)
-#pragma unroll
-            for (int db = 0; db < DB; ++db) {
-                dv[db] = T::mma(frag_t<DP>(tile[buf][1], 16 * h, db, lane), pw[h], dv[db]);
-                dk[db] = T::mma(frag_t<DP>(tile[buf][0], 16 * h, db, lane), dw[h], dk[db]);
-            }
-    };
-    if (n < end) {
-        fetch(n, 0);
-        take(n, 0);
-        int buf = 0, before = 2;
-        for (; n < end; ++n) {
-            const int next = before == 2 ? (buf == 0 ? 1 : 0) : 3 - buf - before;
-            if (n + 1 < end) fetch(n + 1, next);
-            const int t0 = token_of(n);
-            if (!idle && t0 < mine.hi && t0 + RT > mine.lo) {
-                const bool edge = !seen_by_all(w0, w0 + 32, t0);
-                f32x16 p = (f32x16)0.f, d = (f32x16)0.f;
-#pragma unroll
-                for (int ks = 0; ks < KS; ++ks) {
-                    p = T::mma(frag_r<DP>(tile[buf][0], 0, ks, lane), k[ks], p);
-                    d = T::mma(frag_r<DP>(tile[buf][1], 0, ks, lane), v[ks], d);
-                }
-                if (held) add(before);
+    registers_loaded();
+    if (begin < end) {
+        int t0 = ft, tn = fn, slot = 0;
+        for (int x = 0; x < AHEAD; ++x) fetch(x);
+        take(t0, 0);
+        for (int n = begin; n < end; ++n) {
+            fetch(slot == 0 ? RING - 1 : slot - 1);       // the slot of the tile before
+            const int x0 = t0 + 32 * half;
+            const short *const qt = lds + slot * SLOT + half * 32 * DP, *const gt = qt + RT * DP;
+            if (!idle && x0 < mine.hi && x0 + 32 > mine.lo) {
+                // dP starts from -dO.O
+                f32x16 p = (f32x16)0.f, d;
 #pragma unroll
                 for (int i4 = 0; i4 < 4; ++i4) {
-                    const int r = c_row(4 * i4, lane);
-                    const float4 l = *(const float4 *)&stat[buf][0][r], e = *(const float4 *)&stat[buf][1][r];
-                    const float ls[4] = {l.x, l.y, l.z, l.w}, de[4] = {e.x, e.y, e.z, e.w};
+                    const float4 e = *(const float4 *)&stat[slot][half][wave][1][c_row(4 * i4, lane)];
+                    d[4 * i4] = e.x; d[4 * i4 + 1] = e.y; d[4 * i4 + 2] = e.z; d[4 * i4 + 3] = e.w;
+                }
+#pragma unroll
+                for (int ks = 0; ks < KS; ++ks) {
+                    p = T::mma(frag_r<DP>(qt, 0, ks, lane), k[ks], p);
+                    d = T::mma(frag_r<DP>(gt, 0, ks, lane), V_LDS ? frag_r<DP>(vt, 32 * kw, ks, lane) : v[V_LDS ? 0 : ks], d);
+                }
+#pragma unroll
+                for (int i4 = 0; i4 < 4; ++i4) {
+                    const float4 l = *(const float4 *)&stat[slot][half][wave][0][c_row(4 * i4, lane)];
+                    const float ls[4] = {l.x, l.y, l.z, l.w};
 #pragma unroll
                     for (int j = 0; j < 4; ++j) {
                         const int i = 4 * i4 + j;
-                        p[i] = __builtin_amdgcn_exp2f(__builtin_fmaf(p[i], c, LIFT - ls[j]));
-                        d[i] = p[i] * (d[i] - de[j]);
+                        p[i] = __builtin_amdgcn_exp2f(__builtin_fmaf(p[i], c, ls[j]));
+                        d[i] *= p[i];
                     }
                 }
-                if (edge) {
-                    const uint32_t bits = (uint32_t)(below(to - t0) & ~below(from - t0)) >> (4 * (lane >> 5));
+                if (x0 < all_wave.x || x0 + 32 > all_wave.y) {
+                    const uint32_t bits = (uint32_t)(below(to - x0) & ~below(from - x0)) >> (4 * (lane >> 5));
 #pragma unroll
                     for (int i = 0; i < 16; ++i) {
                         p[i] = pick(bits, c_row(i, 0), p[i], 0.f);
@@ -295,46 +316,76 @@ template <class T, int DP> __global__ __launch_bounds__(NT, DP == 128 ? 1 : 2) v
                 unit.fit<T, DB>(d, dk);
 #pragma unroll
                 for (int h = 0; h < 2; ++h) {
-                    pw[h] = as_operand<T>(p, h);
-                    dw[h] = as_operand<T>(d, h);
+                    const s16x8 pw = as_operand<T>(p, h), dw = as_operand<T>(d, h);
+#pragma unroll
+                    for (int db = 0; db < DB; ++db) {
+                        dv[db] = T::mma(frag_t<DP>(gt, 16 * h, db, lane), pw, dv[db]);
+                        dk[db] = T::mma(frag_t<DP>(qt, 16 * h, db, lane), dw, dk[db]);
+                    }
                 }
-                held = true;
-            } else if (held) {
-                add(before);
-                held = false;
             }
-            if (n + 1 < end) take(n + 1, next);
-            before = buf;
-            buf = next;
+            if (++tn == a.group) {
+                tn = 0;
+                t0 += RT;
+            }
+            slot = slot + 1 < RING ? slot + 1 : 0;
+            if (n + 1 < end) take(t0, slot);
         }
-        if (held) add(before);
+        arrived();      // nothing may come into LDS later: it is used otherwise
+    }
+    const float v_by = T::narrow ? 0x1p-12f : 1.f, k_by = T::narrow ? a.scale * 0x1p-12f * unit.u : a.scale;
+#pragma unroll
+    for (int db = 0; db < DB; ++db) {
+        dk[db] *= k_by;
+        dv[db] *= v_by;
+    }
+    if (HALVES == 2) {
+        float *const sums = (float *)lds + kw * 64 * DB * 16 + lane;
+#pragma unroll
+        for (int w = 0; w < 2; ++w) {
+            __syncthreads();
+            f32x16 (&x)[DB] = w ? dv : dk;
+            if (half == 1) {
+#pragma unroll
+                for (int db = 0; db < DB; ++db)
+#pragma unroll
+                    for (int i = 0; i < 16; ++i) sums[64 * (16 * db + i)] = x[db][i];
+            }
+            __syncthreads();
+            if (half == 0) {
+#pragma unroll
+                for (int db = 0; db < DB; ++db)
+#pragma unroll
+                    for (int i = 0; i < 16; ++i) x[db][i] += sums[64 * (16 * db + i)];
+            }
+        }
+        if (half == 1) return;
     }
     const int64_t row = s.k0 + kept;
-    const float v_by = T::narrow ? 0x1p-12f : 1.f, k_by = T::narrow ? a.scale * 0x1p-12f * unit.u : a.scale;
     if (cut) {     // fp32 sums of this part, for join_keys
-        float *to_part = a.part_out + ((((int64_t)it.group * a.split + at_tile) * a.parts + it.part) * 256 + 32 * wave + (lane & 31)) * a.dim;
+        float *to_part = a.part_out + ((((int64_t)it.group * a.split + at_tile) * a.parts + it.part) * 256 + 32 * kw + (lane & 31)) * a.dim;
 #pragma unroll
         for (int db = 0; db < DB; ++db)
 #pragma unroll
             for (int i = 0; i < 16; i += 4) {
                 const int x = 32 * db + c_row(i, lane);
                 if (x >= a.dim) continue;
-                *(float4 *)(to_part + x) = make_float4(dk[db][i] * k_by, dk[db][i + 1] * k_by, dk[db][i + 2] * k_by, dk[db][i + 3] * k_by);
-                *(float4 *)(to_part + (int64_t)128 * a.dim + x) = make_float4(dv[db][i] * v_by, dv[db][i + 1] * v_by, dv[db][i + 2] * v_by, dv[db][i + 3] * v_by);
+                *(float4 *)(to_part + x) = make_float4(dk[db][i], dk[db][i + 1], dk[db][i + 2], dk[db][i + 3]);
+                *(float4 *)(to_part + (int64_t)128 * a.dim + x) = make_float4(dv[db][i], dv[db][i + 1], dv[db][i + 2], dv[db][i + 3]);
             }
         return;
     }
-    store_rows<T, DB>(dv, v_by, a.dv.p, row * a.dv.row + (int64_t)hk * a.dv.head, a.dim, valid, lane);
-    store_rows<T, DB>(dk, k_by, a.dk.p, row * a.dk.row + (int64_t)hk * a.dk.head, a.dim, valid, lane);
+    store_rows<T, DB>(dv, 1.f, a.dv.p, row * a.dv.row + (int64_t)hk * a.dv.head, a.dim, valid, lane);
+    store_rows<T, DB>(dk, 1.f, a.dk.p, row * a.dk.row + (int64_t)hk * a.dk.head, a.dim, valid, lane);
 }
 
 // the parts of the key tiles that were cut, summed in their order: a block to 8 keys of a tile, 32 lanes to a key, 4 values each
-template <class T> __global__ __launch_bounds__(NT) void join_keys(AttendArgs a) {
+template <class T> __global__ __launch_bounds__(NT) void join_keys(AttendArgs a, int rt) {
     const int group = blockIdx.x / (16 * a.split), at_tile = blockIdx.x / 16 % a.split, k0 = at_tile * 128;
     const int b = group / a.kv_heads, hk = group % a.kv_heads, in = blockIdx.x % 16 * 8 + threadIdx.x / 32, x = threadIdx.x % 32 * 4;
     const Sequence s = sequence_of(a, b);
     if (k0 + in >= s.nk || x >= a.dim) return;
-    const KeyTile t = key_tile(a, s, k0, min(k0 + 128, s.nk));
+    const KeyTile t = key_tile(a, s, k0, min(k0 + 128, s.nk), rt);
     if (t.count <= a.chunk) return;
     const int parts = (t.count + a.chunk - 1) / a.chunk;
     const float *from = a.part_out + ((((int64_t)group * a.split + at_tile) * a.parts) * 256 + in) * a.dim + x;
@@ -349,28 +400,24 @@ template <class T> __global__ __launch_bounds__(NT) void join_keys(AttendArgs a)
     *(u32x2 *)(a.dv.p + 2 * (row * a.dv.row + (int64_t)hk * a.dv.head + x)) = (u32x2){T::pack(v.x, v.y), T::pack(v.z, v.w)};
 }
 
-// How grad_keys is cut.  A block has a CU to itself at head sizes above 64, half of one below: 256 or 512 at a time.  With a window all key
-// tiles have about the same rows, but those of the sinks, which all later tokens see: these are cut to the others' size.  Without, the
-// tiles are cut where they are too few to even out their lengths.
+// How grad_keys is cut.  A block has a CU to itself at head sizes above 64, half of one below: 256 or 512 at a time.  Key tiles whose
+// rows are more than an even share of the work are cut into parts of that size where there are too few tiles to even it out; with a
+// window all have about the same rows but those of the sinks, which all later tokens see.
 void cut_keys(AttendArgs &a, int64_t max_k) {
-    const int64_t tiles = cdiv(max_k, 128), items = tiles * a.groups, slots = a.dim > 64 ? 256 : 512;
-    const int64_t longest = cdiv(a.max_q, RT) * a.group, windowed = (cdiv((int64_t)a.window + 128, RT) + 1) * a.group;
+    const int64_t tiles = cdiv(max_k, 128), items = tiles * a.groups, slots = a.dim > 64 ? 256 : 512, rt = rows_of_tile(a.dim > 64 ? 128 : 64);
+    const int64_t longest = cdiv(a.max_q, rt) * a.group;
+    int64_t usual = longest;
+    int64_t work = items * longest / (a.causal ? 2 : 1);
+    if (a.window) usual = std::min(longest, (cdiv((int64_t)a.window + 128, rt) + 1) * a.group);
+    const int64_t sinks = usual < longest ? std::min(tiles, cdiv(a.sinks, 128)) : 0;
+    if (usual < longest) work = std::min(work, items * usual + sinks * a.groups * longest);
     a.tiles = (int)tiles;
-    a.split = 0;
-    a.parts = 1;
-    a.chunk = 0;
-    if (a.window && windowed < longest) {
-        a.split = (int)std::min(tiles, cdiv(a.sinks, 128));
-        a.chunk = (int)windowed;
-    } else if (items < 2 * slots) {
-        a.split = (int)tiles;
-        a.chunk = (int)std::max<int64_t>(8, cdiv(items * longest / (a.causal ? 2 : 1), slots));
-    }
-    if (a.split) a.parts = (int)cdiv(longest, a.chunk);
-    if (a.parts <= 1) {
-        a.parts = 1;
-        a.split = 0;
-    }
+    a.chunk = (int)std::max<int64_t>(8, cdiv(work, slots));
+    if (sinks && a.chunk > usual) a.chunk = (int)usual;
+    a.split = (int)(a.chunk < usual && items < 2 * slots ? tiles : sinks);
+    if (a.split == sinks && a.split < tiles && a.chunk < usual) a.chunk = (int)usual;
+    a.parts = a.split ? (int)cdiv(longest, a.chunk) : 1;
+    if (a.parts == 1) a.split = 0;
 }
 
 int64_t stat_floats(const AttendArgs &a) { return cdiv(2 * a.total_q * a.heads, 64) * 64; }
@@ -387,10 +434,10 @@ template <class T, int DP> void launch(AttendArgs a, int64_t max_k, hipStream_t 
     if (max_k && a.total_k) {
         cut_keys(a, max_k);
         const int64_t blocks = attend_blocks(a, (int64_t)a.tiles * a.parts);
-        grad_keys<T, DP><<<dim3((uint32_t)blocks), NT, 0, st>>>(a);
+        grad_keys<T, DP><<<dim3((uint32_t)blocks), DP == 128 ? 512 : 256, 0, st>>>(a);
         F3M_HIP(hipGetLastError());
         if (a.split) {
-            join_keys<T><<<dim3((uint32_t)((int64_t)a.groups * a.split * 16)), NT, 0, st>>>(a);
+            join_keys<T><<<dim3((uint32_t)((int64_t)a.groups * a.split * 16)), NT, 0, st>>>(a, rows_of_tile(DP));
             F3M_HIP(hipGetLastError());
         }
     }
