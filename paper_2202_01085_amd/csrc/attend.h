@@ -38,7 +38,7 @@ struct AttendArgs {
     // gradient
     Rows dout, dq, dk, dv;
     float *stat;                              // (2, heads, rows of q): -log2 of the row's sum (-inf: empty row), -dO.O
-    int split;                                // key tiles of a group that may be cut into parts; chunk is in row tiles there
+    int split, usual;                         // key tiles of a group that may be cut into parts, chunk row tiles each; parts of tiles without sinks
 };
 
 using s16x4 = __attribute__((ext_vector_type(4))) short;

@@ -156,14 +156,15 @@ template <class T, int DP> __global__ __launch_bounds__(NT, 2) void grad_rows(At
     store_rows<T, DB>(acc, by, a.dq.p, (int64_t)(s.q0 + token) * a.dq.row + (int64_t)head * a.dq.head, a.dim, valid, lane);
 }
 
-// A block of grad_keys: 128 keys of a group and the row tiles that see them, `rt` tokens of one head each: the heads of the group for
-// the first tokens, then for the next.  Blocks begin with different heads: rows of one head lie a multiple of its size apart, so that
-// blocks that all read the same head would all wait for a few channels of the caches.
+// A block of grad_keys: 128 keys of a group and the row tiles that see them, RT tokens of one head each: the heads of the group for the
+// last tokens, then for those before, so that the blocks of a group, which with causal order all see the last tokens, read the same rows
+// at the same time.
+constexpr int RT = 64;
 struct KeyTile {
     int lo, hi, count;    // tokens [lo, hi), row tiles of all heads
 };
 // tokens that see keys of [from, to) are one interval: keys of the sinks stay visible to all later tokens
-__device__ __forceinline__ KeyTile key_tile(const AttendArgs &a, const Sequence &s, int from, int to, int rt) {
+__device__ __forceinline__ KeyTile key_tile(const AttendArgs &a, const Sequence &s, int from, int to) {
     const int off = s.nk - s.nq, nq = min(s.nq, a.max_q);
     KeyTile t;
     t.lo = 0;
@@ -172,34 +173,39 @@ __device__ __forceinline__ KeyTile key_tile(const AttendArgs &a, const Sequence 
         t.lo = min(max(from - off, 0), nq);
         if (a.window && from >= a.sinks) t.hi = max(t.lo, (int)min((int64_t)nq, (int64_t)to - 1 + a.window - off));
     }
-    t.count = (t.hi - t.lo + rt - 1) / rt * a.group;
+    t.count = (t.hi - t.lo + RT - 1) / RT * a.group;
     return t;
 }
-
-// rows of a tile of grad_keys, by head size
-constexpr int rows_of_tile(int dp) { return dp == 128 ? 64 : 32; }
 
 // dK, dV: 32 keys to a wave, whose sums stay in registers; tiles of q and dO come through a ring in LDS, two or more under way while one
 // is worked on.  Head sizes above 64: the sums alone are 128 registers, so that two waves to a SIMD, which the exponentials of one
 // need to run under the products of the other, leave room for k only and v stays in LDS.  There a block has eight waves, two to the same
-// keys, each with every other 32 rows; their sums are added at the end.
+// keys, each with half of a tile's rows; their sums are added at the end.  Below, a wave takes all 64 rows of a tile.
 template <class T, int DP> __global__ __launch_bounds__(DP == 128 ? 512 : 256, 2) void grad_keys(AttendArgs a) {
-    constexpr int KS = DP / 16, DB = DP / 32, HALVES = DP == 128 ? 2 : 1, WAVES = 4 * HALVES, THREADS = 64 * WAVES, RT = rows_of_tile(DP);
+    constexpr int KS = DP / 16, DB = DP / 32, HALVES = DP == 128 ? 2 : 1, SUB = 2 / HALVES, WAVES = 4 * HALVES, THREADS = 64 * WAVES;
     constexpr bool V_LDS = DP == 128;
-    constexpr int AHEAD = DP == 128 ? 2 : 4, RING = AHEAD + 1, SLOT = 2 * RT * DP;
+    constexpr int AHEAD = 2, RING = AHEAD + 1, SLOT = 2 * RT * DP;
     using Src = Tile2<T, DP, RT, WAVES>;
     __shared__ __attribute__((aligned(1024))) short lds[RING * SLOT + (V_LDS ? 128 * DP : 0)];
-    __shared__ __attribute__((aligned(256))) float stat[RING][HALVES][WAVES][2][32];   // a copy to a wave, so that all waves have the same loads under way
+    __shared__ __attribute__((aligned(256))) float stat[RING][2][WAVES][2][32];   // a copy to a wave, so that all waves have the same loads under way
     short *const vt = lds + RING * SLOT;
-    const Item it = block_of(a, blockIdx.x);
+    Item it = block_of(a, blockIdx.x);
     if (it.group >= a.groups) return;
     const int b = it.group / a.kv_heads, hk = it.group % a.kv_heads;
     const Sequence s = sequence_of(a, b);
-    const int at_tile = a.tiles - 1 - it.tile, k0 = at_tile * 128;   // the first keys have most rows
+    // the first keys have most rows: their tiles come first.  Items past the usual parts of all tiles are the sinks' other parts
+    int at_tile = a.tiles - 1 - it.tile;
+    if (it.part >= a.usual) {
+        const int x = (it.part - a.usual) * a.tiles + at_tile, more = a.parts - a.usual;
+        at_tile = x / more;
+        it.part = a.usual + x % more;
+        if (at_tile >= (a.sinks + 127) / 128) return;
+    }
+    const int k0 = at_tile * 128;
     if (k0 >= s.nk) return;
     const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6), kw = wave & 3, half = wave >> 2;
     const int off = s.nk - s.nq;                                     // position of token 0
-    const KeyTile t = key_tile(a, s, k0, min(k0 + 128, s.nk), RT);
+    const KeyTile t = key_tile(a, s, k0, min(k0 + 128, s.nk));
     const bool cut = at_tile < a.split && t.count > a.chunk;
     if (!cut && it.part > 0) return;
     const int begin = cut ? it.part * a.chunk : 0, end = cut ? min(t.count, begin + a.chunk) : t.count;
@@ -210,7 +216,7 @@ template <class T, int DP> __global__ __launch_bounds__(DP == 128 ? 512 : 256, 2
     // tokens [from, to) see this lane's key
     const int from = !valid ? t.hi : a.causal ? max(key - off, 0) : 0;
     const int to = a.causal && a.window && key >= a.sinks ? (int)min((int64_t)t.hi, (int64_t)key + a.window - off) : t.hi;
-    const KeyTile mine = key_tile(a, s, w0, min(w0 + 32, s.nk), RT);     // of the wave: it has nothing to do elsewhere
+    const KeyTile mine = key_tile(a, s, w0, min(w0 + 32, s.nk));     // of the wave: it has nothing to do elsewhere
     // tokens [all.x, all.y) see all keys x .. y - 1
     auto seen_by_all = [&](int x, int y) {
         if (y > s.nk) return make_int2(0, 0);
@@ -236,10 +242,10 @@ template <class T, int DP> __global__ __launch_bounds__(DP == 128 ? 512 : 256, 2
     for (int db = 0; db < DB; ++db) { dk[db] = (f32x16)0.f; dv[db] = (f32x16)0.f; }
     Unit unit{LEAST_UNIT};
 
-    // the next tile to load: tokens ft .. of head fh, the fn-th of the group for these tokens
+    // the next tile to load: tokens ft .. of head fh; the last tiles of tokens end at t.hi, the first may begin before t.lo
     Src src;
     src.start(nullptr, a.q.row, nullptr, a.dout.row, a.dim, wave, lane);
-    int fn = begin % a.group, fh = (fn + at_tile) % a.group, ft = t.lo + begin / a.group * RT, fetched = begin;
+    int fh = begin % a.group, ft = t.hi - (begin / a.group + 1) * RT, fetched = begin;
     const char *const q_base = a.q.p + 2 * ((int64_t)s.q0 * a.q.row + (int64_t)hk * a.group * a.q.head);
     const char *const g_base = a.dout.p + 2 * ((int64_t)s.q0 * a.dout.row + (int64_t)hk * a.group * a.dout.head);
     const float *const stats = a.stat + ((int64_t)(lane < 32 ? 0 : a.heads) + hk * a.group) * a.total_q + s.q0;
@@ -247,26 +253,26 @@ template <class T, int DP> __global__ __launch_bounds__(DP == 128 ? 512 : 256, 2
     auto fetch = [&](int slot) {
         src.base[0] = q_base + 2 * fh * a.q.head;
         src.base[1] = g_base + 2 * fh * a.dout.head;
-        src.issue(ft, t.hi, a.dim, lds + slot * SLOT, lds + slot * SLOT + RT * DP, wave);
+        const int from = max(ft, 0);                   // a tile that would begin before the sequence begins with it
+        src.issue(from, t.hi, a.dim, lds + slot * SLOT, lds + slot * SLOT + RT * DP, wave);
 #pragma unroll
-        for (int h = 0; h < HALVES; ++h)
-            word_to_lds(stats + (int64_t)fh * a.total_q + min(ft + 32 * h + (lane & 31), t.hi - 1), lds_address((const short *)stat[slot][h][wave]));
-        if (++fetched < end) {
-            fh = fh + 1 < a.group ? fh + 1 : 0;
-            if (++fn == a.group) {
-                fn = 0;
-                ft += RT;
-            }
+        for (int h = 0; h < 2; ++h)
+            word_to_lds(stats + (int64_t)fh * a.total_q + min(from + 32 * h + (lane & 31), t.hi - 1), lds_address((const short *)stat[slot][h][wave]));
+        if (++fetched < end && ++fh == a.group) {
+            fh = 0;
+            ft -= RT;
         }
     };
-    constexpr int LOADS = 2 * Src::COUNT + HALVES;    // of a wave to a tile; HALVES of a wave that a small tile leaves nothing to
-    // waits for the loads of a tile, the AHEAD - 1 tiles after it stay under way; q and dO are cleaned where the mask cuts it for the block
-    // (rows with an odd value have such a stat)
+    constexpr int LOADS = 2 * Src::COUNT + 2;    // of a wave to a tile
+    static_assert(Src::STEP <= RT, "every wave has rows of a tile to load");
+    // waits for the loads of a tile, the AHEAD - 1 tiles after it stay under way; where the mask cuts it for the block, q and dO are cleaned
+    // if some row has an odd value: such rows have an odd stat, but for rows that see nothing (-inf)
     auto take = [&](int t0, int slot) {
-        if (Src::STEP > RT && wave * Src::RPI >= RT) arrived<(AHEAD - 1) * HALVES>();
-        else arrived<(AHEAD - 1) * LOADS>();
+        arrived<(AHEAD - 1) * LOADS>();
         __syncthreads();
         if (t0 >= all_block.x && t0 + RT <= all_block.y) return;
+        const float x = stat[slot][0][wave][lane >> 5][lane & 31], y = stat[slot][1][wave][lane >> 5][lane & 31];
+        if (!__any(!(fabsf(x) < __builtin_inff() && fabsf(y) < __builtin_inff()))) return;
         clean_tile<T, DP, RT, THREADS>(lds + slot * SLOT, tid);
         clean_tile<T, DP, RT, THREADS>(lds + slot * SLOT + RT * DP, tid);
         __syncthreads();
@@ -274,59 +280,77 @@ template <class T, int DP> __global__ __launch_bounds__(DP == 128 ? 512 : 256, 2
 
     registers_loaded();
     if (begin < end) {
-        int t0 = ft, tn = fn, slot = 0;
+        int t0 = max(ft, 0), tt = ft, th = fh, slot = 0;
         for (int x = 0; x < AHEAD; ++x) fetch(x);
         take(t0, 0);
         for (int n = begin; n < end; ++n) {
             fetch(slot == 0 ? RING - 1 : slot - 1);       // the slot of the tile before
             const int x0 = t0 + 32 * half;
-            const short *const qt = lds + slot * SLOT + half * 32 * DP, *const gt = qt + RT * DP;
-            if (!idle && x0 < mine.hi && x0 + 32 > mine.lo) {
-                // dP starts from -dO.O
-                f32x16 p = (f32x16)0.f, d;
+            if (!idle && x0 < mine.hi && x0 + 32 * SUB > mine.lo) {
+                f32x16 p[SUB], d[SUB];
 #pragma unroll
-                for (int i4 = 0; i4 < 4; ++i4) {
-                    const float4 e = *(const float4 *)&stat[slot][half][wave][1][c_row(4 * i4, lane)];
-                    d[4 * i4] = e.x; d[4 * i4 + 1] = e.y; d[4 * i4 + 2] = e.z; d[4 * i4 + 3] = e.w;
+                for (int y = 0; y < SUB; ++y) {
+                    p[y] = (f32x16)0.f;
+#pragma unroll
+                    for (int i4 = 0; i4 < 4; ++i4) {      // dP starts from -dO.O
+                        const float4 e = *(const float4 *)&stat[slot][half + y][wave][1][c_row(4 * i4, lane)];
+                        d[y][4 * i4] = e.x; d[y][4 * i4 + 1] = e.y; d[y][4 * i4 + 2] = e.z; d[y][4 * i4 + 3] = e.w;
+                    }
                 }
+                const short *const qt = lds + slot * SLOT + half * 32 * DP, *const gt = qt + RT * DP;
 #pragma unroll
                 for (int ks = 0; ks < KS; ++ks) {
-                    p = T::mma(frag_r<DP>(qt, 0, ks, lane), k[ks], p);
-                    d = T::mma(frag_r<DP>(gt, 0, ks, lane), V_LDS ? frag_r<DP>(vt, 32 * kw, ks, lane) : v[V_LDS ? 0 : ks], d);
-                }
+                    const s16x8 vk = V_LDS ? frag_r<DP>(vt, 32 * kw, ks, lane) : v[V_LDS ? 0 : ks];
 #pragma unroll
-                for (int i4 = 0; i4 < 4; ++i4) {
-                    const float4 l = *(const float4 *)&stat[slot][half][wave][0][c_row(4 * i4, lane)];
-                    const float ls[4] = {l.x, l.y, l.z, l.w};
-#pragma unroll
-                    for (int j = 0; j < 4; ++j) {
-                        const int i = 4 * i4 + j;
-                        p[i] = __builtin_amdgcn_exp2f(__builtin_fmaf(p[i], c, ls[j]));
-                        d[i] *= p[i];
+                    for (int y = 0; y < SUB; ++y) {
+                        p[y] = T::mma(frag_r<DP>(qt, 32 * y, ks, lane), k[ks], p[y]);
+                        d[y] = T::mma(frag_r<DP>(gt, 32 * y, ks, lane), vk, d[y]);
                     }
                 }
-                if (x0 < all_wave.x || x0 + 32 > all_wave.y) {
-                    const uint32_t bits = (uint32_t)(below(to - x0) & ~below(from - x0)) >> (4 * (lane >> 5));
 #pragma unroll
-                    for (int i = 0; i < 16; ++i) {
-                        p[i] = pick(bits, c_row(i, 0), p[i], 0.f);
-                        d[i] = pick(bits, c_row(i, 0), d[i], 0.f);
+                for (int y = 0; y < SUB; ++y)
+#pragma unroll
+                    for (int i4 = 0; i4 < 4; ++i4) {
+                        const float4 l = *(const float4 *)&stat[slot][half + y][wave][0][c_row(4 * i4, lane)];
+                        const float ls[4] = {l.x, l.y, l.z, l.w};
+#pragma unroll
+                        for (int j = 0; j < 4; ++j) {
+                            const int i = 4 * i4 + j;
+                            p[y][i] = __builtin_amdgcn_exp2f(__builtin_fmaf(p[y][i], c, ls[j]));
+                            d[y][i] *= p[y][i];
+                        }
+                    }
+                // tokens of this tile that count: a tile cut short at the front repeats tokens of the one after it
+                const int last = min(to, tt + RT), least = max(from, t0);
+                if (x0 < all_wave.x || x0 + 32 * SUB > all_wave.y || t0 != tt) {
+#pragma unroll
+                    for (int y = 0; y < SUB; ++y) {
+                        const uint32_t bits = (uint32_t)(below(last - x0 - 32 * y) & ~below(least - x0 - 32 * y)) >> (4 * (lane >> 5));
+#pragma unroll
+                        for (int i = 0; i < 16; ++i) {
+                            p[y][i] = pick(bits, c_row(i, 0), p[y][i], 0.f);
+                            d[y][i] = pick(bits, c_row(i, 0), d[y][i], 0.f);
+                        }
                     }
                 }
-                unit.fit<T, DB>(d, dk);
 #pragma unroll
-                for (int h = 0; h < 2; ++h) {
-                    const s16x8 pw = as_operand<T>(p, h), dw = as_operand<T>(d, h);
+                for (int y = 0; y < SUB; ++y) {
+                    unit.fit<T, DB>(d[y], dk);
 #pragma unroll
-                    for (int db = 0; db < DB; ++db) {
-                        dv[db] = T::mma(frag_t<DP>(gt, 16 * h, db, lane), pw, dv[db]);
-                        dk[db] = T::mma(frag_t<DP>(qt, 16 * h, db, lane), dw, dk[db]);
+                    for (int h = 0; h < 2; ++h) {
+                        const s16x8 pw = as_operand<T>(p[y], h), dw = as_operand<T>(d[y], h);
+#pragma unroll
+                        for (int db = 0; db < DB; ++db) {
+                            dv[db] = T::mma(frag_t<DP>(gt, 32 * y + 16 * h, db, lane), pw, dv[db]);
+                            dk[db] = T::mma(frag_t<DP>(qt, 32 * y + 16 * h, db, lane), dw, dk[db]);
+                        }
                     }
                 }
             }
-            if (++tn == a.group) {
-                tn = 0;
-                t0 += RT;
+            if (++th == a.group) {
+                th = 0;
+                tt -= RT;
+                t0 = max(tt, 0);
             }
             slot = slot + 1 < RING ? slot + 1 : 0;
             if (n + 1 < end) take(t0, slot);
@@ -380,12 +404,12 @@ template <class T, int DP> __global__ __launch_bounds__(DP == 128 ? 512 : 256, 2
 }
 
 // the parts of the key tiles that were cut, summed in their order: a block to 8 keys of a tile, 32 lanes to a key, 4 values each
-template <class T> __global__ __launch_bounds__(NT) void join_keys(AttendArgs a, int rt) {
+template <class T> __global__ __launch_bounds__(NT) void join_keys(AttendArgs a) {
     const int group = blockIdx.x / (16 * a.split), at_tile = blockIdx.x / 16 % a.split, k0 = at_tile * 128;
     const int b = group / a.kv_heads, hk = group % a.kv_heads, in = blockIdx.x % 16 * 8 + threadIdx.x / 32, x = threadIdx.x % 32 * 4;
     const Sequence s = sequence_of(a, b);
     if (k0 + in >= s.nk || x >= a.dim) return;
-    const KeyTile t = key_tile(a, s, k0, min(k0 + 128, s.nk), rt);
+    const KeyTile t = key_tile(a, s, k0, min(k0 + 128, s.nk));
     if (t.count <= a.chunk) return;
     const int parts = (t.count + a.chunk - 1) / a.chunk;
     const float *from = a.part_out + ((((int64_t)group * a.split + at_tile) * a.parts) * 256 + in) * a.dim + x;
@@ -404,20 +428,27 @@ template <class T> __global__ __launch_bounds__(NT) void join_keys(AttendArgs a,
 // rows are more than an even share of the work are cut into parts of that size where there are too few tiles to even it out; with a
 // window all have about the same rows but those of the sinks, which all later tokens see.
 void cut_keys(AttendArgs &a, int64_t max_k) {
-    const int64_t tiles = cdiv(max_k, 128), items = tiles * a.groups, slots = a.dim > 64 ? 256 : 512, rt = rows_of_tile(a.dim > 64 ? 128 : 64);
-    const int64_t longest = cdiv(a.max_q, rt) * a.group;
-    int64_t usual = longest;
-    int64_t work = items * longest / (a.causal ? 2 : 1);
-    if (a.window) usual = std::min(longest, (cdiv((int64_t)a.window + 128, rt) + 1) * a.group);
+    const int64_t tiles = cdiv(max_k, 128), items = tiles * a.groups, slots = a.dim > 64 ? 256 : 512;
+    const int64_t longest = std::max<int64_t>(1, cdiv(a.max_q, RT) * a.group);
+    int64_t usual = longest, work = items * longest / (a.causal ? 2 : 1);
+    if (a.window) usual = std::min(longest, (cdiv((int64_t)a.window + 128, RT) + 1) * a.group);
     const int64_t sinks = usual < longest ? std::min(tiles, cdiv(a.sinks, 128)) : 0;
     if (usual < longest) work = std::min(work, items * usual + sinks * a.groups * longest);
+    int64_t chunk = std::max<int64_t>(4, cdiv(work, slots));
+    const bool all = chunk < usual && items < 2 * slots;
+    if (!all) chunk = usual;
     a.tiles = (int)tiles;
-    a.chunk = (int)std::max<int64_t>(8, cdiv(work, slots));
-    if (sinks && a.chunk > usual) a.chunk = (int)usual;
-    a.split = (int)(a.chunk < usual && items < 2 * slots ? tiles : sinks);
-    if (a.split == sinks && a.split < tiles && a.chunk < usual) a.chunk = (int)usual;
-    a.parts = a.split ? (int)cdiv(longest, a.chunk) : 1;
+    a.chunk = (int)chunk;
+    a.split = (int)(all ? tiles : sinks);
+    a.usual = (int)cdiv(usual, chunk);
+    a.parts = (int)std::max<int64_t>(a.usual, a.split ? cdiv(longest, chunk) : 1);
     if (a.parts == 1) a.split = 0;
+}
+
+// items of a group: the usual parts of all tiles, the other parts of the sinks' tiles (in rows of `tiles`, as block_of counts)
+int64_t key_items(const AttendArgs &a) {
+    const int64_t sinks = a.parts > a.usual ? std::min<int64_t>(a.tiles, cdiv(a.sinks, 128)) : 0;
+    return (int64_t)a.tiles * (a.usual + cdiv(sinks * (a.parts - a.usual), a.tiles));
 }
 
 int64_t stat_floats(const AttendArgs &a) { return cdiv(2 * a.total_q * a.heads, 64) * 64; }
@@ -433,11 +464,11 @@ template <class T, int DP> void launch(AttendArgs a, int64_t max_k, hipStream_t 
     }
     if (max_k && a.total_k) {
         cut_keys(a, max_k);
-        const int64_t blocks = attend_blocks(a, (int64_t)a.tiles * a.parts);
+        const int64_t blocks = attend_blocks(a, key_items(a));
         grad_keys<T, DP><<<dim3((uint32_t)blocks), DP == 128 ? 512 : 256, 0, st>>>(a);
         F3M_HIP(hipGetLastError());
         if (a.split) {
-            join_keys<T><<<dim3((uint32_t)((int64_t)a.groups * a.split * 16)), NT, 0, st>>>(a, rows_of_tile(DP));
+            join_keys<T><<<dim3((uint32_t)((int64_t)a.groups * a.split * 16)), NT, 0, st>>>(a);
             F3M_HIP(hipGetLastError());
         }
     }
