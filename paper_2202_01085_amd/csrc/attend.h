@@ -5,7 +5,7 @@
 // and the results C[(i % 4) + 8 (i / 4) + 4 (l / 32)][l % 32], i = 0..15.  So a block of results whose columns stay (queries,
 // say) is the B operand of the next product as it lies in the registers, if that product takes its 16 summands in the order
 //   slot (l / 32, j)  <->  row 4 (l / 32) + j % 4 + 8 (j / 4)
-// and its A operand is read in the same order: two transposing LDS reads of four rows each (frag_t).  No value crosses lanes.
+// and its A operand is read in the same order: two transposing LDS reads of four rows each (column).  No value crosses lanes.
 #pragma once
 #include "common.h"
 
@@ -96,8 +96,8 @@ void run_attend_grad(AttendArgs a, int64_t max_k, bool f16, void *workspace, hip
 void run_cache_rows(const f3m_cache &c, bool f16, const int64_t *slot, int64_t tokens, const f3m_rows &k, const f3m_rows &v, bool write,
                     hipStream_t st);
 
-// ---- tiles in LDS: rows of DP values, their 16-byte pieces exchanged so that neither 8 rows read at one piece (frag_r) nor
-// 4 rows read at two neighbouring ones (frag_t) meet in a bank ----
+// ---- tiles in LDS: rows of DP values, their 16-byte pieces exchanged so that neither 8 rows read at one piece (row) nor
+// 4 rows read at two neighbouring ones (column) meet in a bank ----
 template <int DP> __device__ __forceinline__ int piece_swap(int r) {
     if (DP == 128) return ((r & 7) << 1) ^ ((r >> 3) & 1);
     if (DP == 64) return (r & 6) ^ ((r >> 3) & 1);
@@ -106,17 +106,47 @@ template <int DP> __device__ __forceinline__ int piece_swap(int r) {
 template <int DP> __device__ __forceinline__ int tile_at(int r, int piece) {   // in values
     return r * DP + ((piece ^ piece_swap<DP>(r)) << 3);
 }
-// A operand whose rows are rows of the tile: rows base .. base + 31, dimensions 16 ks .. 16 ks + 15
-template <int DP> __device__ __forceinline__ s16x8 frag_r(const short *tile, int base, int ks, int lane) {
-    return *(const s16x8 *)(tile + tile_at<DP>(base + (lane & 31), 2 * ks + (lane >> 5)));
-}
+using lds_short = __attribute__((address_space(3))) short;
 using lds_s16x4 = __attribute__((address_space(3))) s16x4;
-// A operand whose rows are dimensions 32 db .. 32 db + 31 and whose summands are the tile's rows base .. base + 15, in the order above
-template <int DP> __device__ __forceinline__ s16x8 frag_t(const short *tile, int base, int db, int lane) {
-    const int i = lane & 15, r = base + 4 * (lane >> 5) + (i >> 2), piece = 4 * db + 2 * ((lane >> 4) & 1) + ((i & 3) >> 1), in = (i & 1) << 2;
-    s16x4 x = __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds_s16x4 *)(tile + tile_at<DP>(r, piece) + in));
-    s16x4 y = __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds_s16x4 *)(tile + tile_at<DP>(r + 8, piece) + in));
-    return __builtin_shufflevector(x, y, 0, 1, 2, 3, 4, 5, 6, 7);
+using lds_s16x8 = __attribute__((address_space(3))) s16x8;
+__device__ __forceinline__ uint32_t lds_address(const short *p) { return (uint32_t)(uintptr_t)(const lds_short *)p; }
+
+// Where a lane reads operands of a tile.  Exchanged pieces make the addresses of other pieces exclusive ors, and rows 32 (or 16) further have
+// the same exchange, so they are offsets that the instruction holds: one register to a tile, one operation to a piece.
+template <int DP> struct LaneReads {
+    uint32_t r, t;       // bytes from the tile's start (aligned to a row of pieces) for row() and column()
+    __device__ void start(int lane) {
+        r = 2 * tile_at<DP>(lane & 31, lane >> 5);
+        const int i = lane & 15;
+        t = 2 * (tile_at<DP>(4 * (lane >> 5) + (i >> 2), 2 * ((lane >> 4) & 1) + ((i & 3) >> 1)) + ((i & 1) << 2));
+    }
+    // A operand whose rows are rows base .. base + 31 of the tile (base a multiple of 32): dimensions 16 ks .. 16 ks + 15
+    __device__ s16x8 row(uint32_t tile, int base, int ks) const {
+        return *(const lds_s16x8 *)(uintptr_t)(((tile + r) ^ (32 * ks)) + 2 * DP * base);
+    }
+    // A operand whose rows are dimensions 32 db .. 32 db + 31 and whose summands are rows base .. base + 15 (base a multiple of 16) of the
+    // tile, in the order above: four rows to a read, transposed on the way
+    __device__ s16x8 column(uint32_t tile, int base, int db) const {
+        constexpr uint32_t EIGHT = DP == 32 ? 32 : 16;   // what the exchange of a row 8 further adds
+        const s16x4 x = __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds_s16x4 *)(uintptr_t)(((tile + t) ^ (64 * db)) + 2 * DP * base));
+        const s16x4 y = __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds_s16x4 *)(uintptr_t)(((tile + t) ^ (64 * db) ^ EIGHT) + 2 * DP * (base + 8)));
+        return __builtin_shufflevector(x, y, 0, 1, 2, 3, 4, 5, 6, 7);
+    }
+};
+// Products whose operands come from LDS, read AHEAD of their use: read(i) gives the operand of product i, use(i, operand) makes it.  The
+// order is fixed for the scheduler, which would otherwise read each operand just before its product and wait; arithmetic may move across.
+__device__ __forceinline__ void keep_order() { __builtin_amdgcn_sched_barrier(0x406); }   // vector and scalar arithmetic may cross
+template <int COUNT, int AHEAD, class Read, class Use> __device__ __forceinline__ void products(Read &&read, Use &&use) {
+    s16x8 x[AHEAD];
+#pragma unroll
+    for (int i = 0; i < AHEAD && i < COUNT; ++i) x[i] = read(i);
+    keep_order();
+#pragma unroll
+    for (int i = 0; i < COUNT; ++i) {
+        use(i, x[i % AHEAD]);
+        if (i + AHEAD < COUNT) x[i % AHEAD] = read(i + AHEAD);
+        keep_order();
+    }
 }
 
 // row of result i of a lane
@@ -284,8 +314,6 @@ template <int LEFT = 0> __device__ __forceinline__ void arrived() { asm volatile
 // Waits for loads that came back in registers, where the compiler sees it: it would otherwise wait at their first use inside a loop, and
 // there for all loads under way, the next tiles' too
 __device__ __forceinline__ void registers_loaded() { __builtin_amdgcn_s_waitcnt(0x0f70); }   // vmcnt(0)
-using lds_short = __attribute__((address_space(3))) short;
-__device__ __forceinline__ uint32_t lds_address(const short *p) { return (uint32_t)(uintptr_t)(const lds_short *)p; }
 
 // Tiles of N rows from two tensors (keys and values, say) with fixed strides, for a block of WAVES waves
 template <class T, int DP, int N, int WAVES = 4> struct Tile2 {

@@ -111,16 +111,16 @@ template <class T, int DP> struct Rows32 {
         spoil = 0.f;
     }
 
-    // NB blocks of 32 keys from key0 on, whose rows lie in LDS from row 0 on.  edge: the mask cuts the tile for some row, or `good` (rows
+    // NB blocks of 32 keys from key0 on, whose k and v lie in LDS at kt and vt.  edge: the mask cuts the tile for some row, or `good` (rows
     // in pages of the cache) or `odd` (rows whose infinities or NaN in v are cleaned away) say something
     template <int NB>
-    __device__ __forceinline__ void step(const short *kt, const short *vt, int key0, bool edge, uint64_t good, uint64_t odd, const Limits &mine, int sinks,
+    __device__ __forceinline__ void step(const LaneReads<DP> &at, uint32_t kt, uint32_t vt, int key0, bool edge, uint64_t good, uint64_t odd, const Limits &mine, int sinks,
                                          float c, int lane) {
         f32x16 s[NB];
 #pragma unroll
-        for (int kb = 0; kb < NB; ++kb)
-#pragma unroll
-            for (int ks = 0; ks < KS; ++ks) s[kb] = T::mma(frag_r<DP>(kt, 32 * kb, ks, lane), q[ks], ks ? s[kb] : (f32x16)0.f);
+        for (int kb = 0; kb < NB; ++kb) s[kb] = (f32x16)0.f;
+        // key blocks in turn: two chains of products
+        products<NB * KS, 4>([&](int i) { return at.row(kt, 32 * (i % NB), i / NB); }, [&](int i, s16x8 x) { s[i % NB] = T::mma(x, q[i / NB], s[i % NB]); });
         if (edge) {
             const uint64_t seen = seen_bits(mine, sinks, key0) & good, bits = seen >> (4 * (lane >> 5));
             if (seen & odd) spoil = __builtin_nanf("");
@@ -145,21 +145,25 @@ template <class T, int DP> struct Rows32 {
                 for (int i = 0; i < 16; ++i) o[db][i] *= by;
         }
         const float base = m == NO_KEY ? 0.f : LIFT - m * c;
-#pragma unroll
-        for (int kb = 0; kb < NB; ++kb) {
+        auto weigh = [&](int kb, int from, int to) {
             float sum = 0.f;
 #pragma unroll
-            for (int i = 0; i < 16; ++i) {
+            for (int i = from; i < to; ++i) {
                 s[kb][i] = __builtin_amdgcn_exp2f(__builtin_fmaf(s[kb][i], c, base));
                 sum += s[kb][i];
             }
             l += sum;
+        };
+        weigh(0, 0, 16);
 #pragma unroll
-            for (int h = 0; h < 2; ++h) {
-                const s16x8 w = as_operand<T>(s[kb], h);
-#pragma unroll
-                for (int db = 0; db < DB; ++db) o[db] = T::mma(frag_t<DP>(vt, 32 * kb + 16 * h, db, lane), w, o[db]);
-            }
+        for (int kb = 0; kb < NB; ++kb) {
+            const s16x8 w[2] = {as_operand<T>(s[kb], 0), as_operand<T>(s[kb], 1)};
+            // the exponentials of the next block run under the products of this one
+            products<2 * DB, 2>([&](int i) { return at.column(vt, 32 * kb + 16 * (i / DB), i % DB); },
+                                [&](int i, s16x8 x) {
+                                    o[i % DB] = T::mma(x, w[i / DB], o[i % DB]);
+                                    if (kb + 1 < NB) weigh(kb + 1 < NB ? kb + 1 : 0, 16 * i / (2 * DB), 16 * (i + 1) / (2 * DB));
+                                });
         }
     }
     // the logarithm of the row's sum, in natural units
@@ -226,12 +230,14 @@ template <class T, int DP, bool E8> __global__ __launch_bounds__(NT, 2) void att
     const float c = a.scale * LOG2E;
     auto whole = [&](int key0) { return key0 + KT <= first.hi && (key0 >= last.lo || key0 + KT <= a.sinks); };
 
+    LaneReads<DP> at;
+    at.start(lane);
     Row r;
     r.start(a, a.q.p, (int64_t)(s.q0 + token) * a.q.row + (int64_t)head * a.q.head, lane);
     auto step = [&](int buf, int key0, uint64_t ok, uint64_t odd) {
         const bool none = idle || key0 >= wlast.hi || (key0 + KT <= wfirst.lo && key0 >= a.sinks);
         const bool full = key0 + KT <= wfirst.hi && (key0 >= wlast.lo || key0 + KT <= a.sinks) && ok == ~0ull && odd == 0;
-        if (!none) r.template step<2>(tile[buf][0], tile[buf][1], key0, !full, ok, odd, mine, a.sinks, c, lane);
+        if (!none) r.template step<2>(at, lds_address(tile[buf][0]), lds_address(tile[buf][1]), key0, !full, ok, odd, mine, a.sinks, c, lane);
     };
     registers_loaded();
     if (n < end) {
@@ -336,6 +342,8 @@ template <class T, int DP, bool E8> __global__ __launch_bounds__(NT, 2) void att
     const Limits mine = limits_of(a, s, token);
     const float c = a.scale * LOG2E;
 
+    LaneReads<DP> at;
+    at.start(lane);
     Row r;
     r.start(a, a.q.p, (int64_t)(s.q0 + token) * a.q.row + (int64_t)head * a.q.head, lane);
     registers_loaded();
@@ -354,7 +362,7 @@ template <class T, int DP, bool E8> __global__ __launch_bounds__(NT, 2) void att
                 good = good_pages(a, s, b, tiles[n + 4] * N, lane);
             }
             __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");   // LDS does a wave's accesses in their order: nothing to wait for
-            r.template step<1>(kt, vt, key0, !whole, ok, odd, mine, a.sinks, c, lane);
+            r.template step<1>(at, lds_address(kt), lds_address(vt), key0, !whole, ok, odd, mine, a.sinks, c, lane);
             __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");
         }
     }

@@ -100,14 +100,16 @@ template <class T, int DP> __global__ __launch_bounds__(NT, 2) void grad_rows(At
 #pragma unroll
     for (int db = 0; db < DB; ++db) acc[db] = (f32x16)0.f;
     Unit unit{LEAST_UNIT};
+    LaneReads<DP> at;
+    at.start(lane);
 
-    auto block = [&](const short *kt, const short *vt, int kb, int key0, bool edge) {
+    auto block = [&](uint32_t kt, uint32_t vt, int kb, int key0, bool edge) {
         f32x16 p = (f32x16)0.f, d = (f32x16)delta;     // dP starts from -dO.O
-#pragma unroll
-        for (int ks = 0; ks < KS; ++ks) {
-            p = T::mma(frag_r<DP>(kt, 32 * kb, ks, lane), q[ks], p);
-            d = T::mma(frag_r<DP>(vt, 32 * kb, ks, lane), g[ks], d);
-        }
+        products<2 * KS, 4>([&](int i) { return at.row(i % 2 ? vt : kt, 32 * kb, i / 2); },
+                            [&](int i, s16x8 x) {
+                                if (i % 2) d = T::mma(x, g[i / 2], d);
+                                else p = T::mma(x, q[i / 2], p);
+                            });
 #pragma unroll
         for (int i = 0; i < 16; ++i) d[i] = __builtin_amdgcn_exp2f(__builtin_fmaf(p[i], c, less)) * d[i];
         if (edge) {
@@ -116,12 +118,8 @@ template <class T, int DP> __global__ __launch_bounds__(NT, 2) void grad_rows(At
             for (int i = 0; i < 16; ++i) d[i] = pick(bits, c_row(i, 0), d[i], 0.f);
         }
         unit.fit<T, DB>(d, acc);
-#pragma unroll
-        for (int h = 0; h < 2; ++h) {
-            const s16x8 w = as_operand<T>(d, h);
-#pragma unroll
-            for (int db = 0; db < DB; ++db) acc[db] = T::mma(frag_t<DP>(kt, 32 * kb + 16 * h, db, lane), w, acc[db]);
-        }
+        const s16x8 w[2] = {as_operand<T>(d, 0), as_operand<T>(d, 1)};
+        products<2 * DB, 2>([&](int i) { return at.column(kt, 32 * kb + 16 * (i / DB), i % DB); }, [&](int i, s16x8 x) { acc[i % DB] = T::mma(x, w[i / DB], acc[i % DB]); });
     };
 
     registers_loaded();
@@ -146,8 +144,8 @@ template <class T, int DP> __global__ __launch_bounds__(NT, 2) void grad_rows(At
             const bool none = idle || key0 >= wlast.hi || (key0 + KT <= wfirst.lo && key0 >= a.sinks);
             const bool full = key0 + KT <= wfirst.hi && (key0 >= wlast.lo || key0 + KT <= a.sinks);
             if (!none) {
-                block(tile[buf][0], tile[buf][1], 0, key0, !full);
-                block(tile[buf][0], tile[buf][1], 1, key0, !full);
+                block(lds_address(tile[buf][0]), lds_address(tile[buf][1]), 0, key0, !full);
+                block(lds_address(tile[buf][0]), lds_address(tile[buf][1]), 1, key0, !full);
             }
             if (n + 1 < tiles.count) take(n + 1, buf ^ 1);
         }
@@ -241,6 +239,8 @@ template <class T, int DP> __global__ __launch_bounds__(DP == 128 ? 512 : 256, 2
 #pragma unroll
     for (int db = 0; db < DB; ++db) { dk[db] = (f32x16)0.f; dv[db] = (f32x16)0.f; }
     Unit unit{LEAST_UNIT};
+    LaneReads<DP> at;
+    at.start(lane);
 
     // the next tile to load: tokens ft .. of head fh; the last tiles of tokens end at t.hi, the first may begin before t.lo
     Src src;
@@ -297,15 +297,22 @@ template <class T, int DP> __global__ __launch_bounds__(DP == 128 ? 512 : 256, 2
                         d[y][4 * i4] = e.x; d[y][4 * i4 + 1] = e.y; d[y][4 * i4 + 2] = e.z; d[y][4 * i4 + 3] = e.w;
                     }
                 }
-                const short *const qt = lds + slot * SLOT + half * 32 * DP, *const gt = qt + RT * DP;
-#pragma unroll
-                for (int ks = 0; ks < KS; ++ks) {
-                    const s16x8 vk = V_LDS ? frag_r<DP>(vt, 32 * kw, ks, lane) : v[V_LDS ? 0 : ks];
-#pragma unroll
-                    for (int y = 0; y < SUB; ++y) {
-                        p[y] = T::mma(frag_r<DP>(qt, 32 * y, ks, lane), k[ks], p[y]);
-                        d[y] = T::mma(frag_r<DP>(gt, 32 * y, ks, lane), vk, d[y]);
-                    }
+                const uint32_t qt = lds_address(lds) + 2 * (slot * SLOT + half * 32 * DP), gt = qt + 2 * RT * DP;
+                s16x8 vk[KS];
+                if (V_LDS) {      // dP first, with v read ahead too, then S
+                    products<2 * KS, 4>([&](int i) { return i % 2 ? at.row(gt, 0, i / 2) : at.row(lds_address(vt), 32 * kw, i / 2); },
+                                        [&](int i, s16x8 x) {
+                                            if (i % 2) d[0] = T::mma(x, vk[i / 2], d[0]);
+                                            else vk[i / 2] = x;
+                                        });
+                    products<KS, 4>([&](int i) { return at.row(qt, 0, i); }, [&](int i, s16x8 x) { p[0] = T::mma(x, k[i], p[0]); });
+                } else {
+                    products<2 * SUB * KS, 4>([&](int i) { return at.row(i % 2 ? gt : qt, 32 * (i / 2 % SUB), i / 2 / SUB); },
+                                              [&](int i, s16x8 x) {
+                                                  const int y = i / 2 % SUB, ks = i / 2 / SUB;
+                                                  if (i % 2) d[y] = T::mma(x, v[V_LDS ? 0 : ks], d[y]);
+                                                  else p[y] = T::mma(x, k[ks], p[y]);
+                                              });
                 }
 #pragma unroll
                 for (int y = 0; y < SUB; ++y)
@@ -336,15 +343,13 @@ template <class T, int DP> __global__ __launch_bounds__(DP == 128 ? 512 : 256, 2
 #pragma unroll
                 for (int y = 0; y < SUB; ++y) {
                     unit.fit<T, DB>(d[y], dk);
-#pragma unroll
-                    for (int h = 0; h < 2; ++h) {
-                        const s16x8 pw = as_operand<T>(p[y], h), dw = as_operand<T>(d[y], h);
-#pragma unroll
-                        for (int db = 0; db < DB; ++db) {
-                            dv[db] = T::mma(frag_t<DP>(gt, 32 * y + 16 * h, db, lane), pw, dv[db]);
-                            dk[db] = T::mma(frag_t<DP>(qt, 32 * y + 16 * h, db, lane), dw, dk[db]);
-                        }
-                    }
+                    const s16x8 pw[2] = {as_operand<T>(p[y], 0), as_operand<T>(p[y], 1)}, dw[2] = {as_operand<T>(d[y], 0), as_operand<T>(d[y], 1)};
+                    products<4 * DB, 2>([&](int i) { return at.column(i % 2 ? qt : gt, 32 * y + 16 * (i / 2 / DB), i / 2 % DB); },
+                                        [&](int i, s16x8 x) {
+                                            const int h = i / 2 / DB, db = i / 2 % DB;
+                                            if (i % 2) dk[db] = T::mma(x, dw[h], dk[db]);
+                                            else dv[db] = T::mma(x, pw[h], dv[db]);
+                                        });
                 }
             }
             if (++th == a.group) {
