@@ -17,6 +17,11 @@ FLAGS = ["--offload-arch=gfx950", "-O3", "-std=c++17", "-fPIC", "-Wall", "-Wno-u
          # MFMA results go to ordinary VGPRs (gfx950 has a unified file): no v_accvgpr_read per value
          "-mllvm", "-amdgpu-mfma-vgpr-form"]
 
+# attention: the sums of a tile loop are vectors of 16 values; broken into single ones where branches join, as the compiler does by
+# default, they are copied in every round (64 moves and 64 registers at a head size of 128)
+WHOLE_SUMS = ["-mllvm", "-amdgpu-codegenprepare-break-large-phis=false"]
+EXTRA = {"attend.hip": WHOLE_SUMS, "attend_grad.hip": WHOLE_SUMS}
+
 
 def _hipcc():
     for cand in (os.environ.get("HIPCC"), "/opt/rocm/bin/hipcc", "hipcc"):
@@ -31,7 +36,7 @@ def build_lib(verbose=False):
 
     def compile_one(src):
         obj = os.path.join(OBJDIR, src.replace(".hip", ".o"))
-        cmd = [hipcc, *FLAGS, "-c", os.path.join(CSRC, src), "-o", obj]
+        cmd = [hipcc, *FLAGS, *EXTRA.get(src, []), "-c", os.path.join(CSRC, src), "-o", obj]
         if verbose:
             print(" ".join(cmd), flush=True)
         res = subprocess.run(cmd, capture_output=True, text=True)

@@ -145,14 +145,14 @@ template <class T, int DP> struct Rows32 {
                 for (int i = 0; i < 16; ++i) o[db][i] *= by;
         }
         const float base = m == NO_KEY ? 0.f : LIFT - m * c;
+        float sums[2];
         auto weigh = [&](int kb, int from, int to) {
-            float sum = 0.f;
 #pragma unroll
             for (int i = from; i < to; ++i) {
                 s[kb][i] = __builtin_amdgcn_exp2f(__builtin_fmaf(s[kb][i], c, base));
-                sum += s[kb][i];
+                sums[i % 2] = i < 2 ? s[kb][i] : sums[i % 2] + s[kb][i];
             }
-            l += sum;
+            if (to == 16) l += sums[0] + sums[1];
         };
         weigh(0, 0, 16);
 #pragma unroll
