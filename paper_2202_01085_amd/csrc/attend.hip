@@ -111,16 +111,16 @@ template <class T, int DP> struct Rows32 {
         spoil = 0.f;
     }
 
-    // NB blocks of 32 keys from key0 on, whose k and v lie in LDS at kt and vt.  edge: the mask cuts the tile for some row, or `good` (rows
+    // NB blocks of 32 keys from key0 on: read_k(base, ks) is the A operand of k from row `base` on, v lies in LDS at vt.  edge: the mask cuts the tile for some row, or `good` (rows
     // in pages of the cache) or `odd` (rows whose infinities or NaN in v are cleaned away) say something
-    template <int NB>
-    __device__ __forceinline__ void step(const LaneReads<DP> &at, uint32_t kt, uint32_t vt, int key0, bool edge, uint64_t good, uint64_t odd, const Limits &mine, int sinks,
+    template <int NB, class ReadK>
+    __device__ __forceinline__ void step(const LaneReads<DP> &at, ReadK &&read_k, uint32_t vt, int key0, bool edge, uint64_t good, uint64_t odd, const Limits &mine, int sinks,
                                          float c, int lane) {
         f32x16 s[NB];
 #pragma unroll
         for (int kb = 0; kb < NB; ++kb) s[kb] = (f32x16)0.f;
         // key blocks in turn: two chains of products
-        products<NB * KS, 4>([&](int i) { return at.row(kt, 32 * (i % NB), i / NB); }, [&](int i, s16x8 x) { s[i % NB] = T::mma(x, q[i / NB], s[i % NB]); });
+        products<NB * KS, 4>([&](int i) { return read_k(32 * (i % NB), i / NB); }, [&](int i, s16x8 x) { s[i % NB] = T::mma(x, q[i / NB], s[i % NB]); });
         if (edge) {
             const uint64_t seen = seen_bits(mine, sinks, key0) & good, bits = seen >> (4 * (lane >> 5));
             if (seen & odd) spoil = __builtin_nanf("");
@@ -237,7 +237,8 @@ template <class T, int DP, bool E8> __global__ __launch_bounds__(NT, 2) void att
     auto step = [&](int buf, int key0, uint64_t ok, uint64_t odd) {
         const bool none = idle || key0 >= wlast.hi || (key0 + KT <= wfirst.lo && key0 >= a.sinks);
         const bool full = key0 + KT <= wfirst.hi && (key0 >= wlast.lo || key0 + KT <= a.sinks) && ok == ~0ull && odd == 0;
-        if (!none) r.template step<2>(at, lds_address(tile[buf][0]), lds_address(tile[buf][1]), key0, !full, ok, odd, mine, a.sinks, c, lane);
+        const uint32_t kt = lds_address(tile[buf][0]);
+        if (!none) r.template step<2>(at, [&](int base, int ks) { return at.row(kt, base, ks); }, lds_address(tile[buf][1]), key0, !full, ok, odd, mine, a.sinks, c, lane);
     };
     registers_loaded();
     if (n < end) {
@@ -315,11 +316,16 @@ template <class T, int DP, bool E8> __global__ __launch_bounds__(NT, 2) void att
 }
 
 // Few rows (single tokens, short chunks): a work item is 32 rows and a part of the keys; each of the four waves takes every fourth
-// tile of 32 keys through LDS of its own, and the four results are joined at the end.  Bound by the reading of K and V.
-template <class T, int DP, bool E8> __global__ __launch_bounds__(NT, 2) void attend_few(AttendArgs a) {
+// tile of 32 keys through a ring in LDS of its own, and the four results are joined at the end.  Bound by the reading of K and V.
+constexpr int PAGES_MAX = 1024;   // page numbers of a work item
+
+template <class T, int DP, bool E8> __global__ __launch_bounds__(NT, 1) void attend_few(AttendArgs a) {
     using Row = Rows32<T, DP>;
-    constexpr int N = 32;
-    __shared__ __attribute__((aligned(16))) short tile[4][2][N * DP];
+    constexpr int N = 32, BYTES = E8 ? 1 : 2, PIECES = DP * BYTES / 16, RPI = 64 / PIECES, COUNT = N / RPI;   // pieces of a row, rows to an instruction
+    constexpr int RING = E8 ? 3 : 2, TILE = N * DP * BYTES, SLOT = 2 * TILE + (E8 ? 256 : 0), LOADS = 2 * COUNT + (E8 ? 1 : 0);
+    constexpr int OF_WAVE = RING * SLOT + (E8 ? 2 * N * DP : 0);                                           // 8 bits: and a tile of v as 16-bit values
+    __shared__ __attribute__((aligned(1024))) char lds[4 * OF_WAVE];
+    __shared__ int pages[PAGES_MAX];
     __shared__ float joined[4][2][32];
     const Item it = block_of(a, blockIdx.x);
     if (it.group >= a.groups) return;
@@ -330,12 +336,11 @@ template <class T, int DP, bool E8> __global__ __launch_bounds__(NT, 2) void att
     const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6);
     const Limits first = limits_of(a, s, r0 / a.group), last = limits_of(a, s, min(r0 + 31, rows - 1) / a.group);
     const Tiles tiles = tiles_of<N>(first, last, a.sinks);
-    int n = it.part * a.chunk + wave, end = tiles.count;
-    if (a.parts > 1) end = min(end, (it.part + 1) * a.chunk);
+    const int begin = it.part * a.chunk, end = a.parts > 1 ? min(tiles.count, begin + a.chunk) : tiles.count;
     const int row = min(r0 + (lane & 31), rows - 1), token = row / a.group, head = hk * a.group + row % a.group;
     const bool valid = r0 + (lane & 31) < rows;
     const int64_t at_row = (int64_t)(s.q0 + token) * a.heads + head;
-    if (it.part * a.chunk >= tiles.count && it.part > 0) {   // nothing here: the part counts as empty
+    if (begin >= tiles.count && it.part > 0) {   // nothing here: the part counts as empty
         if (wave == 0 && lane < 32 && valid) a.part_lse[(int64_t)it.part * a.total_q * a.heads + at_row] = NO_KEY;
         return;
     }
@@ -346,25 +351,109 @@ template <class T, int DP, bool E8> __global__ __launch_bounds__(NT, 2) void att
     at.start(lane);
     Row r;
     r.start(a, a.q.p, (int64_t)(s.q0 + token) * a.q.row + (int64_t)head * a.q.head, lane);
+    // the page of rows u * sub .. of tile begin + i is pages[i * subs + u]; -1: none
+    const int shift = min(a.page_shift, 5), subs = 32 >> shift;
+    if (a.table) {
+        for (int x = tid; x < (end - begin) * subs; x += NT) {
+            const int j = min(tiles[begin + x / subs] * N + (x % subs << shift), s.nk - 1), page = a.table[(int64_t)b * a.table_row + (j >> a.page_shift)];
+            pages[x] = page >= 0 && page < a.pages ? page : -1;
+        }
+        __syncthreads();
+    }
     registers_loaded();
-    short *kt = tile[wave][0], *vt = tile[wave][1];
+
+    // the exchange of 16-byte pieces of a tile of codes: rows of one piece spread over all banks
+    auto swap = [](int x) { return E8 ? (DP == 128 ? (x >> 1) & 7 : DP == 64 ? (x >> 2) & 3 : (x >> 3) & 1) : piece_swap<DP>(x); };
+    const uint32_t ring = lds_address((const short *)lds) + wave * OF_WAVE, v16 = ring + RING * SLOT;
+    auto fetch = [&](int n, int slot) {
+        const int key0 = tiles[n] * N;
+        const uint32_t to = ring + slot * SLOT;
+#pragma unroll
+        for (int x = 0; x < COUNT; ++x) {
+            const int in = x * RPI + lane / PIECES, j = min(key0 + in, s.nk - 1), y = 16 * ((lane % PIECES) ^ swap(in)), piece = y < BYTES * a.dim ? y : 0;
+            int64_t k, v;
+            if (a.table) {
+                const int page = max(pages[(n - begin) * subs + (in >> shift)], 0);
+                k = v = BYTES * ((((int64_t)page * a.kv_heads + hk) << a.page_shift) + (j & ((1 << a.page_shift) - 1))) * a.dim + piece;
+            } else {
+                k = BYTES * ((int64_t)(s.k0 + j) * a.k.row + (int64_t)hk * a.k.head) + piece;
+                v = BYTES * ((int64_t)(s.k0 + j) * a.v.row + (int64_t)hk * a.v.head) + piece;
+            }
+            to_lds(a.k.p + k, to + 1024 * x);
+            to_lds(a.v.p + v, to + TILE + 1024 * x);
+        }
+        if (E8) {   // four exponents to a lane: of k, then of v; pages hold multiples of 8 rows
+            const int in = 4 * (lane & 7), j = min(key0 + in, (s.nk - 1) & ~3), page = max(pages[(n - begin) * subs + (in >> shift)], 0);
+            const int64_t x = (((int64_t)page * a.kv_heads + hk) << a.page_shift) + (j & ((1 << a.page_shift) - 1));
+            word_to_lds((const float *)((lane & 8 ? a.v_exp : a.k_exp) + x), to + 2 * TILE);
+        }
+    };
+    int n = begin + wave;
     if (n < end) {
-        Stage<T, DP, E8, N, 64> next;
-        next.load(a, s, b, hk, tiles[n] * N, lane);
-        uint64_t good = good_pages(a, s, b, tiles[n] * N, lane);
-        for (; n < end; n += 4) {
+        const int final = n + (end - 1 - n) / 4 * 4;      // the wave's last tile: loaded again past the end, which keeps the count of loads
+        for (int x = 0; x < RING; ++x) fetch(min(n + 4 * x, final), x);
+        for (int slot = 0; n < end; n += 4, slot = slot + 1 < RING ? slot + 1 : 0) {
             const int key0 = tiles[n] * N;
-            const bool whole = key0 + N <= first.hi && (key0 >= last.lo || key0 + N <= a.sinks) && (uint32_t)good == ~0u;
-            const uint64_t odd = next.store(kt, vt, lane, !whole);
-            const uint64_t ok = good;
-            if (n + 4 < end) {
-                next.load(a, s, b, hk, tiles[n + 4] * N, lane);
-                good = good_pages(a, s, b, tiles[n + 4] * N, lane);
+            const uint32_t kt = ring + slot * SLOT, vt = kt + TILE;
+            uint64_t good = ~0ull;
+            if (a.table) good = __ballot(pages[(n - begin) * subs + ((lane & 31) >> shift)] >= 0);
+            const bool whole = key0 + N <= first.hi && (key0 >= last.lo || key0 + N <= a.sinks) && good == ~0ull;
+            arrived<(RING - 1) * LOADS>();
+            uint64_t odd = 0;
+            using lds_piece = __attribute__((address_space(3))) u32x4;
+            if constexpr (E8) {
+                // v as 16-bit values, for transposing reads; k is converted as it is read
+                using lds_byte = __attribute__((address_space(3))) const uint8_t;
+#pragma unroll
+                for (int x = 0; x < COUNT; ++x) {
+                    const int in = x * RPI + lane / PIECES, piece = (lane % PIECES) ^ swap(in);
+                    const u32x4 w = *(lds_piece *)(uintptr_t)(vt + 1024 * x + 16 * lane);
+                    const float scale = __builtin_bit_cast(float, (uint32_t)*(lds_byte *)(uintptr_t)(kt + 2 * TILE + 32 + in) << 23);
+#pragma unroll
+                    for (int h = 0; h < 2; ++h) {
+                        u32x4 y = {T::template codes<false>(w[2 * h], scale), T::template codes<true>(w[2 * h], scale),
+                                   T::template codes<false>(w[2 * h + 1], scale), T::template codes<true>(w[2 * h + 1], scale)};
+                        if (!whole && any_odd<T>(y)) {
+                            y = cleaned<T>(y);
+                            odd |= 1ull << in;
+                        }
+                        *(lds_piece *)(uintptr_t)(v16 + 2 * tile_at<DP>(in, 2 * piece + h)) = y;
+                    }
+                }
+            } else if (!whole) {
+#pragma unroll 2
+                for (int x = 0; x < COUNT; ++x) {
+                    lds_piece *const p = (lds_piece *)(uintptr_t)(vt + 1024 * x + 16 * lane);
+                    const u32x4 w = *p;
+                    if (any_odd<T>(w)) {
+                        *p = cleaned<T>(w);
+                        odd |= 1ull << (x * RPI + lane / PIECES);
+                    }
+                }
+            }
+            if (!whole && __any(odd != 0)) {
+#pragma unroll 1
+                for (int by = 32; by > 0; by >>= 1) odd |= __shfl_xor((unsigned long long)odd, by);
             }
             __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");   // LDS does a wave's accesses in their order: nothing to wait for
-            r.template step<1>(at, lds_address(kt), lds_address(vt), key0, !whole, ok, odd, mine, a.sinks, c, lane);
+            if constexpr (E8) {
+                using lds_byte = __attribute__((address_space(3))) const uint8_t;
+                using lds_codes = __attribute__((address_space(3))) const u32x2;
+                const float scale = __builtin_bit_cast(float, (uint32_t)*(lds_byte *)(uintptr_t)(kt + 2 * TILE + (lane & 31)) << 23);
+                const uint32_t from = kt + (lane & 31) * DP + 16 * swap(lane & 31) + 8 * (lane >> 5);
+                auto read_k = [&](int, int ks) {
+                    const u32x2 w = *(lds_codes *)(uintptr_t)(from ^ (16 * ks));
+                    return __builtin_bit_cast(s16x8, (u32x4){T::template codes<false>(w[0], scale), T::template codes<true>(w[0], scale),
+                                                            T::template codes<false>(w[1], scale), T::template codes<true>(w[1], scale)});
+                };
+                r.template step<1>(at, read_k, v16, key0, !whole, good, odd, mine, a.sinks, c, lane);
+            } else {
+                r.template step<1>(at, [&](int base, int ks) { return at.row(kt, base, ks); }, vt, key0, !whole, good, odd, mine, a.sinks, c, lane);
+            }
             __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");
+            fetch(min(n + 4 * RING, final), slot);
         }
+        arrived();      // LDS is used otherwise from here on
     }
     // join: every wave's o in the common unit, summed over the waves from LDS
     const float all = both_halves_sum(r.l);
@@ -381,7 +470,8 @@ template <class T, int DP, bool E8> __global__ __launch_bounds__(NT, 2) void att
     const float spoil = both_halves_sum(r.spoil);
     const float unit = all == 0.f ? 0.f : __builtin_amdgcn_exp2f((r.m - top) * c), by = spoil + (sum > 0.f ? unit / sum : sum == sum ? 0.f : sum);
     r.m = top;
-    float *mine_o = (float *)tile[wave];       // 32 x DP values, the two tiles' 4 * 32 * DP bytes
+    static_assert(OF_WAVE >= 4 * 32 * DP, "room for 32 x DP values of fp32");
+    float *mine_o = (float *)(lds + wave * OF_WAVE);
 #pragma unroll
     for (int db = 0; db < Row::DB; ++db)
 #pragma unroll
@@ -404,7 +494,7 @@ template <class T, int DP, bool E8> __global__ __launch_bounds__(NT, 2) void att
             float4 t = make_float4(0.f, 0.f, 0.f, 0.f);
 #pragma unroll
             for (int w = 0; w < 4; ++w) {
-                const float4 u = *(const float4 *)((const float *)tile[w] + x * DP + ((((d >> 2) + h) ^ (x & 7)) << 2));
+                const float4 u = *(const float4 *)((const float *)(lds + w * OF_WAVE) + x * DP + ((((d >> 2) + h) ^ (x & 7)) << 2));
                 t.x += u.x; t.y += u.y; t.z += u.z; t.w += u.w;
             }
             y[4 * h] = t.x; y[4 * h + 1] = t.y; y[4 * h + 2] = t.z; y[4 * h + 3] = t.w;
@@ -421,29 +511,31 @@ template <class T, int DP, bool E8> __global__ __launch_bounds__(NT, 2) void att
     }
 }
 
-// The parts of each row joined: 32 lanes to a row, four dimensions each.  Rows of no sequence have no parts and are left alone.
-template <class T> __global__ __launch_bounds__(NT) void join_parts(AttendArgs a) {
-    const int64_t row = (int64_t)blockIdx.x * 8 + threadIdx.x / 32, all = a.total_q * a.heads;
-    if (row >= all) return;
-    const int x = threadIdx.x % 32 * 4;
-    const int64_t token = row / a.heads;
-    const int head = (int)(row % a.heads);
-    if (a.q_offsets) {
-        // the sequence of the token: the last offset not above it
-        int lo = 0, hi = a.batch;
-        while (lo < hi) {
-            const int mid = (lo + hi) / 2;
-            if (a.q_offsets[mid + 1] <= token) lo = mid + 1;
-            else hi = mid;
-        }
-        if (lo == a.batch || token < a.q_offsets[lo]) return;
-        if (token - a.q_offsets[lo] >= a.max_q) return;
-    } else if (token >= a.max_q) {
-        return;
+// whether a row of q and its results belongs to some sequence (and to its first max_q tokens): others have no parts and are left alone
+__device__ __forceinline__ bool in_sequence(const AttendArgs &a, int64_t token) {
+    if (!a.q_offsets) return token < a.max_q;
+    int lo = 0, hi = a.batch;      // the last offset not above the token
+    while (lo < hi) {
+        const int mid = (lo + hi) / 2;
+        if (a.q_offsets[mid + 1] <= token) lo = mid + 1;
+        else hi = mid;
     }
-    float top = NO_KEY;
+    return lo < a.batch && token >= a.q_offsets[lo] && token - a.q_offsets[lo] < a.max_q;
+}
+template <class T> __device__ __forceinline__ void store_joined(const AttendArgs &a, int64_t row, int x, float top, float sum, float4 o) {
+    const float by = sum > 0.f ? 1.f / sum : sum == sum ? 0.f : sum;
+    if (x == 0) a.lse[row] = sum > 0.f ? top + __builtin_amdgcn_logf(sum) * LN2 : sum == sum ? NO_KEY : sum;
+    if (x < a.dim)
+        *(u32x2 *)(a.out.p + 2 * (row / a.heads * a.out.row + row % a.heads * a.out.head + x)) = (u32x2){T::pack(o.x * by, o.y * by), T::pack(o.z * by, o.w * by)};
+}
+
+// The parts of each row joined: 32 lanes to a row, four dimensions each, part after part
+template <class T> __global__ __launch_bounds__(NT) void join_few(AttendArgs a) {
+    const int64_t row = (int64_t)blockIdx.x * 8 + threadIdx.x / 32, all = a.total_q * a.heads;
+    if (row >= all || !in_sequence(a, row / a.heads)) return;
+    const int x = threadIdx.x % 32 * 4;
+    float top = NO_KEY, sum = 0.f;
     for (int p = 0; p < a.parts; ++p) top = fmaxf(top, a.part_lse[p * all + row]);
-    float sum = 0.f;
     float4 o = make_float4(0.f, 0.f, 0.f, 0.f);
     for (int p = 0; p < a.parts; ++p) {
         const float l = a.part_lse[p * all + row];
@@ -455,10 +547,52 @@ template <class T> __global__ __launch_bounds__(NT) void join_parts(AttendArgs a
             o.x += w * u.x; o.y += w * u.y; o.z += w * u.z; o.w += w * u.w;
         }
     }
-    const float by = sum > 0.f ? 1.f / sum : sum == sum ? 0.f : sum;
-    if (x == 0) a.lse[row] = sum > 0.f ? top + __builtin_amdgcn_logf(sum) * LN2 : sum == sum ? NO_KEY : sum;
-    if (x < a.dim)
-        *(u32x2 *)(a.out.p + 2 * (token * a.out.row + (int64_t)head * a.out.head + x)) = (u32x2){T::pack(o.x * by, o.y * by), T::pack(o.z * by, o.w * by)};
+    store_joined<T>(a, row, x, top, sum, o);
+}
+
+// The same for many parts, a block to a row: the parts' weights by all threads, then every eighth part to 32 lanes
+template <class T> __global__ __launch_bounds__(NT) void join_many(AttendArgs a) {
+    __shared__ float weight[NT], most[4], sums[4];
+    __shared__ float4 partial[8][32];
+    const int64_t row = blockIdx.x, all = a.total_q * a.heads;
+    const int tid = threadIdx.x, x = tid % 32 * 4;
+    if (!in_sequence(a, row / a.heads)) return;
+    float top = NO_KEY;
+    for (int p = tid; p < a.parts; p += NT) top = fmaxf(top, a.part_lse[p * all + row]);
+#pragma unroll
+    for (int by = 32; by > 0; by >>= 1) top = fmaxf(top, __shfl_xor(top, by));
+    if (tid % 64 == 0) most[tid / 64] = top;
+    __syncthreads();
+    top = fmaxf(fmaxf(most[0], most[1]), fmaxf(most[2], most[3]));
+    float sum = 0.f;
+    float4 o = make_float4(0.f, 0.f, 0.f, 0.f);
+    for (int p0 = 0; p0 < a.parts; p0 += NT) {
+        const float l = p0 + tid < a.parts ? a.part_lse[(p0 + tid) * all + row] : NO_KEY, w = l == NO_KEY ? 0.f : __builtin_amdgcn_exp2f((l - top) * LOG2E);
+        sum += w;
+        __syncthreads();
+        weight[tid] = l == NO_KEY ? -1.f : w;          // -1: nothing was written for this part
+        __syncthreads();
+        if (x < a.dim)
+#pragma unroll 4
+            for (int p = tid / 32; p < min(NT, a.parts - p0); p += 8) {
+                const float v = weight[p];
+                if (v == -1.f) continue;
+                const float4 u = *(const float4 *)(a.part_out + ((p0 + p) * all + row) * a.dim + x);
+                o.x += v * u.x; o.y += v * u.y; o.z += v * u.z; o.w += v * u.w;
+            }
+    }
+#pragma unroll
+    for (int by = 32; by > 0; by >>= 1) sum += __shfl_xor(sum, by);
+    if (tid % 64 == 0) sums[tid / 64] = sum;
+    partial[tid / 32][tid % 32] = o;
+    __syncthreads();
+    if (tid >= 32) return;
+#pragma unroll
+    for (int p = 1; p < 8; ++p) {
+        const float4 u = partial[p][tid];
+        o.x += u.x; o.y += u.y; o.z += u.z; o.w += u.w;
+    }
+    store_joined<T>(a, row, x, top, (sums[0] + sums[1]) + (sums[2] + sums[3]), o);
 }
 
 // key tiles of `per` rows that a work item of `rows` (token, head) rows may see at most
@@ -473,7 +607,9 @@ template <class T, int DP, bool E8> void launch(const AttendArgs &a, bool few, i
     else attend_many<T, DP, E8><<<dim3((uint32_t)blocks), NT, 0, st>>>(a);
     F3M_HIP(hipGetLastError());
     if (a.parts > 1) {
-        join_parts<T><<<dim3((uint32_t)cdiv(a.total_q * a.heads, 8)), NT, 0, st>>>(a);
+        const int64_t all = a.total_q * a.heads;
+        if (a.parts > 8 && all < 4096) join_many<T><<<dim3((uint32_t)all), NT, 0, st>>>(a);
+        else join_few<T><<<dim3((uint32_t)cdiv(all, 8)), NT, 0, st>>>(a);
         F3M_HIP(hipGetLastError());
     }
 }
@@ -485,14 +621,27 @@ template <class T> void launch_dim(const AttendArgs &a, bool e8, bool few, int64
 }
 
 // Up to 64 rows to a key head go to attend_few.  A long key axis is cut into parts where the rows alone make too few blocks: two
-// blocks fit a CU, 512 the device.
+// blocks of attend_many fit a CU, one of attend_few, whose waves keep 64 KB or more under way.
 bool split(AttendArgs &a, int64_t max_k) {
     const bool few = (int64_t)a.max_q * a.group <= 64;
     const int per = few ? 32 : KT, rows = few ? 32 : 128, least = few ? 16 : 8;
     a.tiles = (int)cdiv((int64_t)a.max_q * a.group, rows);
     const int64_t most = most_tiles(a, max_k, rows, per), items = (int64_t)a.tiles * a.groups;
-    const int64_t want = few ? cdiv(2048, items) : items >= 512 ? 1 : cdiv(1024, items);
-    a.chunk = (int)std::max<int64_t>(cdiv(most, want), std::min<int64_t>(least, most));
+    int64_t parts = 1;
+    if (few) {
+        parts = cdiv(1024, items);
+    } else if (items < 512) {   // the fewest rounds of 512 blocks for the work of one, a part costing some of it
+        double least_cost = 1e30;
+        for (int64_t p = 1; p <= 512; ++p) {
+            const double cost = (double)cdiv(items * p, 512) / (double)p + 0.02 * (double)p * (double)items / 512.0;
+            if (cost < least_cost) {
+                least_cost = cost;
+                parts = p;
+            }
+        }
+    }
+    a.chunk = (int)std::max<int64_t>(cdiv(most, parts), std::min<int64_t>(least, most));
+    if (few) a.chunk = std::min(a.chunk, PAGES_MAX / 4);
     a.parts = (int)cdiv(most, a.chunk);
     return few;
 }
