@@ -382,39 +382,45 @@ def direct_kmvm_xy_rows_f64(X, Y, b, lengthscale, rows, stream=None):
 
 
 # ---- row-normalised products (attention) ----
+# A call on a few rows takes a GPU some microseconds: the checks below ask each tensor for its shape and strides once.
 
-class _On:
-    """The device of the call's tensors made current, and the call's stream: what the binding allocates belongs to that stream."""
-
-    def __init__(self, device, stream):
-        self.stream = torch.cuda.current_stream(device) if stream is None else stream
-        if self.stream.device != device:
-            raise ValueError("the stream is of %s, the tensors are on %s" % (self.stream.device, device))
-        self._scope = torch.cuda.stream(self.stream)     # also makes the stream's device current
-        self.handle = ctypes.c_void_p(self.stream.cuda_stream)
-
-    def __enter__(self):
-        self._scope.__enter__()
-        return self
-
-    def __exit__(self, *e):
-        return self._scope.__exit__(*e)
+_SIXTEEN = (torch.bfloat16, torch.float16)
 
 
-def _rows(t, name, like=None, heads=None, rows=None):
-    """a (rows, heads, head_dim) device tensor, head_dim contiguous, as the library takes it"""
-    if not (isinstance(t, torch.Tensor) and t.is_cuda and t.dim() == 3 and t.dtype in (torch.bfloat16, torch.float16)):
+def _on_stream(device, stream, body):
+    """body(stream handle) with the tensors' device current and the call's stream the current one, so that what the binding allocates
+    belongs to it"""
+    if stream is None:
+        if device.index == torch.cuda.current_device():
+            return body(torch._C._cuda_getCurrentRawStream(device.index))
+        stream = torch.cuda.current_stream(device)
+    elif stream.device != device:
+        raise ValueError("the stream is of %s, the tensors are on %s" % (stream.device, device))
+    with torch.cuda.stream(stream):
+        return body(stream.cuda_stream)
+
+
+def _rows(t, name, dtype=None, device=None, shape=None):
+    """a (rows, heads, head_dim) device tensor, head_dim contiguous, as the library takes it; shape: what it has to be"""
+    if not (isinstance(t, torch.Tensor) and t.is_cuda and t.dim() == 3 and t.dtype in _SIXTEEN):
         raise TypeError("%s must be a device tensor (rows, heads, head_dim) of bfloat16 or float16" % name)
-    if like is not None and (t.dtype != like.dtype or t.device != like.device or t.shape[2] != like.shape[2]):
-        raise ValueError("%s must have the type, the device and the head_dim of the other tensors" % name)
-    if heads is not None and t.shape[1] != heads or rows is not None and t.shape[0] != rows:
-        raise ValueError("%s must have shape (%s, %s, head_dim)" % (name, "rows" if rows is None else rows, "heads" if heads is None else heads))
-    if t.shape[2] > 1 and t.stride(2) != 1:
+    if dtype is not None and (t.dtype != dtype or t.device != device):
+        raise ValueError("%s must have the type and the device of the other tensors" % name)
+    have = t.shape
+    if shape is not None and have != shape:
+        raise ValueError("%s must have shape %s" % (name, tuple(shape)))
+    rows, heads, dim = have
+    row, head, one = t.stride()
+    if one != 1 and dim > 1:
         raise ValueError("%s must be contiguous along head_dim" % name)
-    row, head = t.stride(0) if t.shape[0] > 1 else t.shape[2], t.stride(1) if t.shape[1] > 1 else t.shape[2]
-    if t.numel() and (t.data_ptr() % 16 or row % 8 or head % 8):
+    if rows == 1:
+        row = dim
+    if heads == 1:
+        head = dim
+    at = t.data_ptr()
+    if (at | row << 1 | head << 1) & 15 and rows * heads * dim:
         raise ValueError("%s must be 16-byte aligned, with strides that are multiples of 8" % name)
-    return Rows(t.data_ptr() if t.numel() else None, row, head)
+    return Rows(at or None, row, head)
 
 
 def _device_array(t, name, dtype, device, shape):
@@ -422,49 +428,50 @@ def _device_array(t, name, dtype, device, shape):
         raise TypeError("%s must be a %s tensor on %s" % (name, str(dtype).replace("torch.", ""), device))
     if t.shape != shape or not t.is_contiguous():
         raise ValueError("%s must be contiguous and have shape %s" % (name, tuple(shape)))
-    return t.data_ptr() if t.numel() else None
+    return t.data_ptr() or None
 
 
-def _lse(lse, rows, heads, device):
-    if lse is None:
-        return torch.empty((rows, heads), dtype=torch.float32, device=device)
-    _device_array(lse, "lse", torch.float32, device, (rows, heads))
-    return lse
-
-
-def _attention_args(q, kv_heads, q_offsets, max_q, scale, causal, window, sinks):
-    a = AttentionArgs()
-    a.q = _rows(q, "q")
-    a.dtype, a.heads, a.kv_heads, a.head_dim = DTYPES[q.dtype], q.shape[1], kv_heads, q.shape[2]
-    a.causal, a.window, a.sinks = int(bool(causal)), int(window), int(sinks)
-    a.scale = 1.0 / q.shape[2] ** 0.5 if scale is None and q.shape[2] else float(1.0 if scale is None else scale)
-    a.total_q = q.shape[0]
-    a.max_q = q.shape[0] if max_q is None else int(max_q)
-    a.batch = 1
+def _attention_args(q, shape, rq, rk, rv, kv_heads, total_k, q_offsets, k_offsets, max_q, max_k, scale, causal, window, sinks):
+    rows, heads, dim = shape
+    batch, qo = 1, None
     if q_offsets is not None:
-        a.batch = max(0, q_offsets.numel() - 1)
-        a.q_offsets = _device_array(q_offsets, "q_offsets", torch.int32, q.device, (a.batch + 1,))
-    return a
+        batch = max(0, q_offsets.shape[0] - 1) if q_offsets.dim() == 1 else 0
+        qo = _device_array(q_offsets, "q_offsets", torch.int32, q.device, (batch + 1,))
+    ko = None if k_offsets is None else _device_array(k_offsets, "k_offsets", torch.int32, q.device, (batch + 1,))
+    if scale is None:
+        scale = 1.0 / dim ** 0.5 if dim else 1.0
+    return AttentionArgs(DTYPES[q.dtype], batch, heads, kv_heads, dim, 1 if causal else 0, int(window), int(sinks), scale,
+                         rows if max_q is None else int(max_q), total_k if max_k is None else int(max_k), rows, total_k, qo, ko, rq, rk, rv)
 
 
 def _packed_args(q, k, v, q_offsets, k_offsets, max_q, max_k, scale, causal, window, sinks):
-    a = _attention_args(q, k.shape[1] if isinstance(k, torch.Tensor) and k.dim() == 3 else 0, q_offsets, max_q, scale, causal, window, sinks)
-    a.k = _rows(k, "k", q)
-    a.v = _rows(v, "v", q, k.shape[1], k.shape[0])
-    a.total_k = k.shape[0]
-    a.max_k = k.shape[0] if max_k is None else int(max_k)
+    rq = _rows(q, "q")
+    shape, dtype, device = q.shape, q.dtype, q.device
+    rk = _rows(k, "k", dtype, device)
+    rows, heads, dim = k.shape
+    if dim != shape[2]:
+        raise ValueError("k must have the head_dim of q")
+    rv = _rows(v, "v", dtype, device, k.shape)
     if (q_offsets is None) != (k_offsets is None):
         raise ValueError("q_offsets and k_offsets are given both or neither")
-    if k_offsets is not None:
-        a.k_offsets = _device_array(k_offsets, "k_offsets", torch.int32, q.device, (a.batch + 1,))
-    return a
+    return _attention_args(q, shape, rq, rk, rv, heads, rows, q_offsets, k_offsets, max_q, max_k, scale, causal, window, sinks)
+
+
+def _lse(lse, shape, device):
+    if lse is None:
+        return torch.empty(shape, dtype=torch.float32, device=device)
+    _device_array(lse, "lse", torch.float32, device, shape)
+    return lse
 
 
 def _workspace(call, a, device):
-    need = int(call(ctypes.byref(a)))
-    if need < 0:
-        _check(-need)
-    return (torch.empty(need, dtype=torch.uint8, device=device) if need else None), need
+    need = call(ctypes.byref(a))
+    if need <= 0:
+        if need < 0:
+            _check(-need)
+        return None, None, 0
+    w = torch.empty(need, dtype=torch.uint8, device=device)
+    return w, w.data_ptr(), need
 
 
 def attention(q, k, v, q_offsets=None, k_offsets=None, max_q=None, max_k=None, scale=None, causal=True, window=0, sinks=0, out=None,
@@ -477,30 +484,40 @@ def attention(q, k, v, q_offsets=None, k_offsets=None, max_q=None, max_k=None, s
     nk - nq + i; window > 0: the last `window` of those and the first `sinks`.  scale: 1/sqrt(head_dim) by default.
     lse (rows, heads) float32: logarithms of the sums, -inf where nothing is visible (and out is 0)."""
     a = _packed_args(q, k, v, q_offsets, k_offsets, max_q, max_k, scale, causal, window, sinks)
-    with _On(q.device, stream) as on:
-        out = torch.empty(q.shape, dtype=q.dtype, device=q.device) if out is None else out
-        to = _rows(out, "out", q, q.shape[1], q.shape[0])
-        lse = _lse(lse, q.shape[0], q.shape[1], q.device)
-        w, need = _workspace(lib().f3m_attention_workspace, a, q.device)
-        _check(lib().f3m_attention(ctypes.byref(a), ctypes.byref(to), lse.data_ptr() or None, w.data_ptr() if need else None, need, on.handle))
-    return out, lse
+    device, shape = q.device, q.shape
+
+    def call(handle):
+        o = torch.empty(shape, dtype=q.dtype, device=device) if out is None else out
+        to = _rows(o, "out", q.dtype, device, shape)
+        ls = _lse(lse, shape[:2], device)
+        L = lib()
+        w, at, need = _workspace(L.f3m_attention_workspace, a, device)
+        _check(L.f3m_attention(ctypes.byref(a), ctypes.byref(to), ls.data_ptr() or None, at, need, handle))
+        return o, ls
+
+    return _on_stream(device, stream, call)
 
 
 def attention_grad(dout, q, k, v, out, lse, q_offsets=None, k_offsets=None, max_q=None, max_k=None, scale=None, causal=True, window=0,
                    sinks=0, dq=None, dk=None, dv=None, stream=None):
     """f3m_attention_grad: (dq, dk, dv) from the gradient dout of out, with the out and lse of attention() and its arguments."""
     a = _packed_args(q, k, v, q_offsets, k_offsets, max_q, max_k, scale, causal, window, sinks)
-    g, o = _rows(dout, "dout", q, q.shape[1], q.shape[0]), _rows(out, "out", q, q.shape[1], q.shape[0])
+    device, dtype, shape = q.device, q.dtype, q.shape
+    g, o = _rows(dout, "dout", dtype, device, shape), _rows(out, "out", dtype, device, shape)
     if lse is None:
         raise TypeError("lse must be that of attention()")
-    lse = _lse(lse, q.shape[0], q.shape[1], q.device)
-    with _On(q.device, stream) as on:
-        got = [torch.empty(x.shape, dtype=x.dtype, device=x.device) if y is None else y for x, y in ((q, dq), (k, dk), (v, dv))]
-        to = [_rows(y, name, q, x.shape[1], x.shape[0]) for y, name, x in zip(got, ("dq", "dk", "dv"), (q, k, v))]
-        w, need = _workspace(lib().f3m_attention_grad_workspace, a, q.device)
-        _check(lib().f3m_attention_grad(ctypes.byref(a), ctypes.byref(g), ctypes.byref(o), lse.data_ptr() or None,
-                                        *(ctypes.byref(t) for t in to), w.data_ptr() if need else None, need, on.handle))
-    return tuple(got)
+    _lse(lse, shape[:2], device)
+
+    def call(handle):
+        got = [torch.empty(x.shape, dtype=dtype, device=device) if y is None else y for x, y in ((q, dq), (k, dk), (v, dv))]
+        to = [_rows(y, name, dtype, device, x.shape) for y, name, x in zip(got, ("dq", "dk", "dv"), (q, k, v))]
+        L = lib()
+        w, at, need = _workspace(L.f3m_attention_grad_workspace, a, device)
+        _check(L.f3m_attention_grad(ctypes.byref(a), ctypes.byref(g), ctypes.byref(o), lse.data_ptr() or None, ctypes.byref(to[0]),
+                                    ctypes.byref(to[1]), ctypes.byref(to[2]), at, need, handle))
+        return tuple(got)
+
+    return _on_stream(device, stream, call)
 
 
 class KVCache:
@@ -533,28 +550,33 @@ class KVCache:
         exp = [torch.full(shape[:3], 127, dtype=torch.uint8, device=device) if dtype == torch.float8_e4m3fn else None for _ in range(2)]
         return cls(zeros(shape, dtype), zeros(shape, dtype), *exp)
 
-    def _move(self, call, k, v, slots, stream):
-        rk, rv = _rows(k, "k"), _rows(v, "v", k, k.shape[1], k.shape[0])
-        if k.shape[1:] != (self._c.kv_heads, self._c.head_dim) or k.device != self.k.device:
+    def _move(self, call, k, v, slots, handle):
+        device, c = self.k.device, self._c
+        rk = _rows(k, "k")
+        shape = k.shape
+        if shape[1:] != (c.kv_heads, c.head_dim) or k.device != device:
             raise ValueError("k and v must have shape (tokens, kv_heads, head_dim) as the cache, and be on its device")
-        at = _device_array(slots, "slots", torch.int64, self.k.device, (k.shape[0],))
-        with _On(self.k.device, stream) as on:
-            _check(call(ctypes.byref(self._c), DTYPES[k.dtype], ctypes.byref(rk), ctypes.byref(rv), at, k.shape[0], on.handle))
+        rv = _rows(v, "v", k.dtype, device, shape)
+        at = _device_array(slots, "slots", torch.int64, device, shape[:1])
+        _check(call(ctypes.byref(c), DTYPES[k.dtype], ctypes.byref(rk), ctypes.byref(rv), at, shape[0], handle))
 
     def write(self, k, v, slots, stream=None):
         """f3m_cache_write: k, v (tokens, kv_heads, head_dim) to slots (tokens) int64, on the device; slots outside the cache are skipped.
         No slot may come twice in a call."""
-        self._move(lib().f3m_cache_write, k, v, slots, stream)
+        _on_stream(self.k.device, stream, lambda handle: self._move(lib().f3m_cache_write, k, v, slots, handle))
 
     def read(self, slots, dtype=None, k=None, v=None, stream=None):
         """f3m_cache_read: (k, v) of the slots, of `dtype` (default: bfloat16 from an 8-bit cache, else the cache's); zeros for slots outside"""
         dtype = (torch.bfloat16 if self._c.held == 2 else self.k.dtype) if dtype is None else dtype
         shape = (slots.numel(), self._c.kv_heads, self._c.head_dim)
-        with _On(self.k.device, stream) as on:
-            k = torch.empty(shape, dtype=dtype, device=self.k.device) if k is None else k
-            v = torch.empty(shape, dtype=dtype, device=self.k.device) if v is None else v
-            self._move(lib().f3m_cache_read, k, v, slots, on.stream)
-        return k, v
+
+        def call(handle):
+            kk = torch.empty(shape, dtype=dtype, device=self.k.device) if k is None else k
+            vv = torch.empty(shape, dtype=dtype, device=self.k.device) if v is None else v
+            self._move(lib().f3m_cache_read, kk, vv, slots, handle)
+            return kk, vv
+
+        return _on_stream(self.k.device, stream, call)
 
     def attention(self, q, table, lengths, q_offsets=None, max_q=None, max_k=None, scale=None, causal=True, window=0, sinks=0, out=None,
                   lse=None, stream=None):
@@ -563,29 +585,39 @@ class KVCache:
         Key j of sequence b lies in page table[b, j // page_size] (int32, on the device), j < lengths[b] (int32, on the device).
         q_offsets as for attention(); without, every sequence has the same number of new tokens (rows of q / sequences).
         max_k: the longest length (default: what the table has room for)."""
-        if not (isinstance(table, torch.Tensor) and table.is_cuda and table.dtype == torch.int32 and table.dim() == 2 and table.device == self.k.device):
+        device, c = self.k.device, self._c
+        if not (isinstance(table, torch.Tensor) and table.is_cuda and table.dtype == torch.int32 and table.dim() == 2 and table.device == device):
             raise TypeError("table must be an int32 tensor (sequences, pages) on the cache's device")
-        if table.numel() and table.shape[1] > 1 and table.stride(1) != 1 or table.stride(0) < table.shape[1] and table.shape[0] > 1:
+        batch, cols = table.shape
+        step, one = table.stride()
+        if batch * cols and (one != 1 and cols > 1 or step < cols and batch > 1):
             raise ValueError("table must be contiguous along the pages")
-        batch = table.shape[0]
-        _rows(q, "q")
-        with _On(self.k.device, stream) as on:
-            if q_offsets is None:
-                if q.shape[0] % max(1, batch):
+        rq = _rows(q, "q")
+        shape = q.shape
+        if q.device != device:
+            raise ValueError("q must be on the cache's device")
+        ln = _device_array(lengths, "lengths", torch.int32, device, (batch,))
+
+        def call(handle):
+            offsets, most = q_offsets, max_q
+            if offsets is None:
+                if shape[0] % max(1, batch):
                     raise ValueError("without q_offsets all sequences have the same number of new tokens")
-                each = q.shape[0] // max(1, batch)
-                q_offsets = torch.arange(batch + 1, dtype=torch.int32, device=self.k.device).mul_(each)
-                max_q = each if max_q is None else max_q
-            a = _attention_args(q, self._c.kv_heads, q_offsets, max_q, scale, causal, window, sinks)
-            if a.batch != batch or q.device != self.k.device:
-                raise ValueError("q_offsets must have one entry more than the table has rows, and q must be on the cache's device")
-            ln = _device_array(lengths, "lengths", torch.int32, self.k.device, (batch,))
-            a.max_k = min(table.shape[1] * self._c.page_size, 2 ** 31 - 65537) if max_k is None else int(max_k)
-            out = torch.empty(q.shape, dtype=q.dtype, device=q.device) if out is None else out
-            to = _rows(out, "out", q, q.shape[1], q.shape[0])
-            lse = _lse(lse, q.shape[0], q.shape[1], q.device)
-            w, need = _workspace(lib().f3m_attention_workspace, a, q.device)
-            _check(lib().f3m_cache_attention(ctypes.byref(self._c), ctypes.byref(a), table.data_ptr() if table.numel() else None,
-                                             max(table.stride(0), table.shape[1]), table.shape[1], ln, ctypes.byref(to), lse.data_ptr() or None,
-                                             w.data_ptr() if need else None, need, on.handle))
-        return out, lse
+                each = shape[0] // max(1, batch)
+                offsets = torch.arange(0, each * batch + 1, max(1, each), dtype=torch.int32, device=device) if each else \
+                    torch.zeros(batch + 1, dtype=torch.int32, device=device)
+                most = each if most is None else most
+            a = _attention_args(q, shape, rq, Rows(), Rows(), c.kv_heads, 0, offsets, None, most, min(cols * c.page_size, 2 ** 31 - 65537) if max_k is None else max_k,
+                                scale, causal, window, sinks)
+            if a.batch != batch:
+                raise ValueError("q_offsets must have one entry more than the table has rows")
+            o = torch.empty(shape, dtype=q.dtype, device=device) if out is None else out
+            to = _rows(o, "out", q.dtype, device, shape)
+            ls = _lse(lse, shape[:2], device)
+            L = lib()
+            w, at, need = _workspace(L.f3m_attention_workspace, a, device)
+            _check(L.f3m_cache_attention(ctypes.byref(c), ctypes.byref(a), table.data_ptr() or None, max(step, cols), cols, ln, ctypes.byref(to),
+                                         ls.data_ptr() or None, at, need, handle))
+            return o, ls
+
+        return _on_stream(device, stream, call)
