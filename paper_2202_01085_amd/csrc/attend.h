@@ -334,16 +334,17 @@ template <class T, int DP, int N, int WAVES = 4> struct Tile2 {
         for (int w = 0; w < 2; ++w)                        // zeros where the tile is wider than the head
             off[w] = piece * 8 >= dim ? NOWHERE : (uint32_t)(row * stride[w] + piece * 16);
     }
-    // rows from row0 on; rows from `end` on give zeros
-    __device__ void issue(int row0, int end, int dim, const short *tx, const short *ty, int wave) const {
+    // rows from row0 on of one tensor; rows from `end` on give zeros
+    template <int W> __device__ void issue_one(int row0, int end, int dim, const short *tile, int wave) const {
         if (N < STEP && wave * RPI >= N) return;
+        const u32x4 buffer = buffer_of(base[W] + (int64_t)row0 * stride[W], (min(end - row0, N) - 1) * stride[W] + 2 * dim);
+        const uint32_t lds = lds_address(tile) + wave * 1024;
 #pragma unroll
-        for (int w = 0; w < 2; ++w) {
-            const u32x4 buffer = buffer_of(base[w] + (int64_t)row0 * stride[w], (min(end - row0, N) - 1) * stride[w] + 2 * dim);
-            const uint32_t lds = lds_address(w ? ty : tx) + wave * 1024;
-#pragma unroll
-            for (int c = 0; c < COUNT; ++c) to_lds(buffer, off[w], (uint32_t)(STEP * c * stride[w]), lds + 1024 * WAVES * c);
-        }
+        for (int c = 0; c < COUNT; ++c) to_lds(buffer, off[W], (uint32_t)(STEP * c * stride[W]), lds + 1024 * WAVES * c);
+    }
+    __device__ void issue(int row0, int end, int dim, const short *tx, const short *ty, int wave) const {
+        issue_one<0>(row0, end, dim, tx, wave);
+        issue_one<1>(row0, end, dim, ty, wave);
     }
 };
 // infinities and NaN of a tile become 0; bits of the rows that had one (a wave's)

@@ -120,7 +120,9 @@ template <class T, int DP> struct Rows32 {
 #pragma unroll
         for (int kb = 0; kb < NB; ++kb) s[kb] = (f32x16)0.f;
         // key blocks in turn: two chains of products
+        __builtin_amdgcn_s_setprio(1);      // the matrix cores to the wave that is at the scores, arithmetic to the other of the SIMD
         products<NB * KS, 4>([&](int i) { return read_k(32 * (i % NB), i / NB); }, [&](int i, s16x8 x) { s[i % NB] = T::mma(x, q[i / NB], s[i % NB]); });
+        __builtin_amdgcn_s_setprio(0);
         if (edge) {
             const uint64_t seen = seen_bits(mine, sinks, key0) & good, bits = seen >> (4 * (lane >> 5));
             if (seen & odd) spoil = __builtin_nanf("");
@@ -165,6 +167,14 @@ template <class T, int DP> struct Rows32 {
                                     if (kb + 1 < NB) weigh(kb + 1 < NB ? kb + 1 : 0, 16 * i / (2 * DB), 16 * (i + 1) / (2 * DB));
                                 });
         }
+    }
+    __device__ bool finite() const {
+        bool all = true;
+#pragma unroll
+        for (int db = 0; db < DB; ++db)
+#pragma unroll
+            for (int i = 0; i < 16; ++i) all &= fabsf(o[db][i]) < __builtin_inff();
+        return all;
     }
     // the logarithm of the row's sum, in natural units
     __device__ float lse(float all, float c) const { return all > 0.f ? (m * c - LIFT + __builtin_amdgcn_logf(all)) * LN2 : all == all ? NO_KEY : all; }
@@ -233,15 +243,19 @@ template <class T, int DP, bool E8> __global__ __launch_bounds__(NT, 2) void att
     LaneReads<DP> at;
     at.start(lane);
     Row r;
-    r.start(a, a.q.p, (int64_t)(s.q0 + token) * a.q.row + (int64_t)head * a.q.head, lane);
-    auto step = [&](int buf, int key0, uint64_t ok, uint64_t odd) {
-        const bool none = idle || key0 >= wlast.hi || (key0 + KT <= wfirst.lo && key0 >= a.sinks);
-        const bool full = key0 + KT <= wfirst.hi && (key0 >= wlast.lo || key0 + KT <= a.sinks) && ok == ~0ull && odd == 0;
-        const uint32_t kt = lds_address(tile[buf][0]);
-        if (!none) r.template step<2>(at, [&](int base, int ks) { return at.row(kt, base, ks); }, lds_address(tile[buf][1]), key0, !full, ok, odd, mine, a.sinks, c, lane);
-    };
-    registers_loaded();
-    if (n < end) {
+    const int begin = n;
+    // Tiles that the mask cuts are not cleaned of infinities and NaN in v at first: if none shows in the results, there was none that
+    // mattered.  Else all is done again with care.
+    auto pass = [&](bool careful) {
+        n = begin;
+        r.start(a, a.q.p, (int64_t)(s.q0 + token) * a.q.row + (int64_t)head * a.q.head, lane);
+        auto step = [&](int buf, int key0, uint64_t ok, uint64_t odd) {
+            const bool none = idle || key0 >= wlast.hi || (key0 + KT <= wfirst.lo && key0 >= a.sinks);
+            const bool full = key0 + KT <= wfirst.hi && (key0 >= wlast.lo || key0 + KT <= a.sinks) && ok == ~0ull && odd == 0;
+            const uint32_t kt = lds_address(tile[buf][0]);
+            if (!none) r.template step<2>(at, [&](int base, int ks) { return at.row(kt, base, ks); }, lds_address(tile[buf][1]), key0, !full, ok, odd, mine, a.sinks, c, lane);
+        };
+        if (n >= end) return;
         if constexpr (E8) {
             Stage<T, DP, E8, KT, NT> next;
             uint64_t good = 0;
@@ -250,17 +264,18 @@ template <class T, int DP, bool E8> __global__ __launch_bounds__(NT, 2) void att
                 if (wave == 0) good = good_pages(a, s, b, tiles[t] * KT, lane);
             };
             auto keep = [&](int t, int buf) {
-                const uint64_t odd = next.store(tile[buf][0], tile[buf][1], tid, !whole(tiles[t] * KT));
-                if (lane == 0) odd_rows[buf][wave] = odd;
+                const uint64_t odd = next.store(tile[buf][0], tile[buf][1], tid, careful && !whole(tiles[t] * KT));
+                if (careful && lane == 0) odd_rows[buf][wave] = odd;
                 if (tid == 0) good_rows[buf] = good;
             };
             fetch(n);
             keep(n, n & 1);
+            registers_loaded();
             __syncthreads();
             for (; n < end; ++n) {
                 const int buf = n & 1;
                 if (n + 1 < end) fetch(n + 1);
-                step(buf, tiles[n] * KT, good_rows[buf], odd_rows[buf][0] | odd_rows[buf][1] | odd_rows[buf][2] | odd_rows[buf][3]);
+                step(buf, tiles[n] * KT, good_rows[buf], careful ? odd_rows[buf][0] | odd_rows[buf][1] | odd_rows[buf][2] | odd_rows[buf][3] : 0);
                 if (n + 1 < end) keep(n + 1, buf ^ 1);
                 __syncthreads();
             }
@@ -273,12 +288,12 @@ template <class T, int DP, bool E8> __global__ __launch_bounds__(NT, 2) void att
                 next_ok = good_pages(a, s, b, tiles[t] * KT, lane);
                 if (t + 1 < end) src.look(a, s, b, tiles[t + 1] * KT);
             };
-            // waits for the loads of tile t; cleans it where the mask cuts it for the block
+            // waits for the loads of tile t
             auto take = [&](int t, int buf) -> uint64_t {
                 arrived();
                 __syncthreads();
                 ok = next_ok;
-                if (whole(tiles[t] * KT) && ok == ~0ull) return 0;
+                if (!careful || (whole(tiles[t] * KT) && ok == ~0ull)) return 0;
                 const uint64_t odd = clean_tile<T, DP, KT>(tile[buf][1], tid);
                 if (lane == 0) odd_rows[buf][wave] = odd;
                 __syncthreads();
@@ -286,6 +301,7 @@ template <class T, int DP, bool E8> __global__ __launch_bounds__(NT, 2) void att
             };
             src.look(a, s, b, tiles[n] * KT);
             fetch(n, n & 1);
+            registers_loaded();
             uint64_t odd = take(n, n & 1);
             for (; n < end; ++n) {
                 const int buf = n & 1;
@@ -294,7 +310,9 @@ template <class T, int DP, bool E8> __global__ __launch_bounds__(NT, 2) void att
                 if (n + 1 < end) odd = take(n + 1, buf ^ 1);
             }
         }
-    }
+    };
+    pass(false);
+    if (__syncthreads_or(!r.finite())) pass(true);
     const float all = both_halves_sum(r.l), by = both_halves_sum(r.spoil) + (all > 0.f ? 1.f / all : all == all ? 0.f : all);
     const int64_t at_row = (int64_t)(s.q0 + token) * a.heads + head;
     if (a.parts > 1) {
