@@ -214,7 +214,7 @@ template <class T, int DP> struct Direct : Tile2<T, DP, KT> {
 
 // Many rows: a work item is 128 rows of one group, the four waves share tiles of 64 keys, two in LDS in turn.  Bound by the matrix cores
 // and by what LDS delivers to them (one operand of each product comes from there).
-template <class T, int DP, bool E8> __global__ __launch_bounds__(NT, 2) void attend_many(AttendArgs a) {
+template <class T, int DP, bool E8> __global__ __launch_bounds__(NT, DP == 128 ? 2 : 3) void attend_many(AttendArgs a) {
     using Row = Rows32<T, DP>;
     constexpr int ROWS = 128;
     __shared__ __attribute__((aligned(1024))) short tile[2][2][KT * DP];
@@ -639,7 +639,7 @@ template <class T> void launch_dim(const AttendArgs &a, bool e8, bool few, int64
 }
 
 // Up to 64 rows to a key head go to attend_few.  A long key axis is cut into parts where the rows alone make too few blocks: two
-// blocks of attend_many fit a CU, one of attend_few, whose waves keep 64 KB or more under way.
+// blocks of attend_many fit a CU (three up to a head size of 64), one of attend_few, whose waves keep 64 KB or more under way.
 bool split(AttendArgs &a, int64_t max_k) {
     const bool few = (int64_t)a.max_q * a.group <= 64;
     const int per = few ? 32 : KT, rows = few ? 32 : 128, least = few ? 16 : 8;
@@ -648,10 +648,10 @@ bool split(AttendArgs &a, int64_t max_k) {
     int64_t parts = 1;
     if (few) {
         parts = cdiv(1024, items);
-    } else if (items < 512) {   // the fewest rounds of 512 blocks for the work of one, a part costing some of it
+    } else if (const int64_t slots = a.dim > 64 ? 512 : 768; items < slots) {   // the fewest rounds of blocks for the work of one, a part costing some of it
         double least_cost = 1e30;
-        for (int64_t p = 1; p <= 512; ++p) {
-            const double cost = (double)cdiv(items * p, 512) / (double)p + 0.02 * (double)p * (double)items / 512.0;
+        for (int64_t p = 1; p <= slots; ++p) {
+            const double cost = (double)cdiv(items * p, slots) / (double)p + 0.02 * (double)p * (double)items / (double)slots;
             if (cost < least_cost) {
                 least_cost = cost;
                 parts = p;
