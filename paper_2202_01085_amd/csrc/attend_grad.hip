@@ -97,19 +97,19 @@ template <class T, int DP> __global__ __launch_bounds__(NT, 2) void grad_rows(At
         q[ks] = __builtin_bit_cast(s16x8, load_piece<DP>(a.q.p, (int64_t)(s.q0 + token) * a.q.row + (int64_t)head * a.q.head, 2 * ks + (lane >> 5), a.dim));
         g[ks] = __builtin_bit_cast(s16x8, load_piece<DP>(a.dout.p, (int64_t)(s.q0 + token) * a.dout.row + (int64_t)head * a.dout.head, 2 * ks + (lane >> 5), a.dim));
     }
-#pragma unroll
-    for (int db = 0; db < DB; ++db) acc[db] = (f32x16)0.f;
     Unit unit{LEAST_UNIT};
     LaneReads<DP> at;
     at.start(lane);
 
     auto block = [&](uint32_t kt, uint32_t vt, int kb, int key0, bool edge) {
         f32x16 p = (f32x16)0.f, d = (f32x16)delta;     // dP starts from -dO.O
+        __builtin_amdgcn_s_setprio(1);      // the matrix cores to the wave that is at the scores, arithmetic to the other of the SIMD
         products<2 * KS, 4>([&](int i) { return at.row(i % 2 ? vt : kt, 32 * kb, i / 2); },
                             [&](int i, s16x8 x) {
                                 if (i % 2) d = T::mma(x, g[i / 2], d);
                                 else p = T::mma(x, q[i / 2], p);
                             });
+        __builtin_amdgcn_s_setprio(0);
 #pragma unroll
         for (int i = 0; i < 16; ++i) d[i] = __builtin_amdgcn_exp2f(__builtin_fmaf(p[i], c, less)) * d[i];
         if (edge) {
@@ -122,21 +122,27 @@ template <class T, int DP> __global__ __launch_bounds__(NT, 2) void grad_rows(At
         products<2 * DB, 2>([&](int i) { return at.column(kt, 32 * kb + 16 * (i / DB), i % DB); }, [&](int i, s16x8 x) { acc[i % DB] = T::mma(x, w[i / DB], acc[i % DB]); });
     };
 
-    registers_loaded();
-    if (tiles.count > 0) {
+    // Tiles that the mask cuts are cleaned of infinities and NaN in k only when some shows in the results (rows that see one have such an
+    // lse, and are NaN either way)
+    auto pass = [&](bool careful) {
+#pragma unroll
+        for (int db = 0; db < DB; ++db) acc[db] = (f32x16)0.f;
+        unit.u = LEAST_UNIT;
+        if (tiles.count == 0) return;
         Tile2<T, DP, KT> src;
         src.start(a.k.p + 2 * ((int64_t)s.k0 * a.k.row + (int64_t)hk * a.k.head), a.k.row, a.v.p + 2 * ((int64_t)s.k0 * a.v.row + (int64_t)hk * a.v.head), a.v.row, a.dim, wave, lane);
         auto fetch = [&](int t, int buf) { src.issue(tiles[t] * KT, s.nk, a.dim, tile[buf][0], tile[buf][1], wave); };
-        // waits for the loads of tile t; k is cleaned where the mask cuts the tile for the block: rows that see an odd k have such an lse
+        // waits for the loads of tile t
         auto take = [&](int t, int buf) {
             arrived();
             __syncthreads();
             const int key0 = tiles[t] * KT;
-            if (key0 + KT <= first.hi && (key0 >= last.lo || key0 + KT <= a.sinks)) return;
+            if (!careful || (key0 + KT <= first.hi && (key0 >= last.lo || key0 + KT <= a.sinks))) return;
             clean_tile<T, DP, KT>(tile[buf][0], tid);
             __syncthreads();
         };
         fetch(0, 0);
+        registers_loaded();
         take(0, 0);
         for (int n = 0; n < tiles.count; ++n) {
             const int buf = n & 1, key0 = tiles[n] * KT;
@@ -149,7 +155,14 @@ template <class T, int DP> __global__ __launch_bounds__(NT, 2) void grad_rows(At
             }
             if (n + 1 < tiles.count) take(n + 1, buf ^ 1);
         }
-    }
+    };
+    pass(false);
+    bool finite = true;
+#pragma unroll
+    for (int db = 0; db < DB; ++db)
+#pragma unroll
+        for (int i = 0; i < 16; ++i) finite &= fabsf(acc[db][i]) < __builtin_inff();
+    if (__syncthreads_or(!finite)) pass(true);
     const float by = T::narrow ? a.scale * unit.u : a.scale;
     store_rows<T, DB>(acc, by, a.dq.p, (int64_t)(s.q0 + token) * a.dq.row + (int64_t)head * a.dq.head, a.dim, valid, lane);
 }
@@ -278,10 +291,10 @@ template <class T, int DP> __global__ __launch_bounds__(DP == 128 ? 512 : 256, 2
         __syncthreads();
     };
 
-    registers_loaded();
     if (begin < end) {
         int t0 = max(ft, 0), tt = ft, th = fh, slot = 0;
         for (int x = 0; x < AHEAD; ++x) fetch(x);
+        registers_loaded();
         take(t0, 0);
         for (int n = begin; n < end; ++n) {
             fetch(slot == 0 ? RING - 1 : slot - 1);       // the slot of the tile before
@@ -298,6 +311,7 @@ template <class T, int DP> __global__ __launch_bounds__(DP == 128 ? 512 : 256, 2
                     }
                 }
                 const uint32_t qt = lds_address(lds) + 2 * (slot * SLOT + half * 32 * DP), gt = qt + 2 * RT * DP;
+                __builtin_amdgcn_s_setprio(1);
                 s16x8 vk[KS];
                 if (V_LDS) {      // dP first, with v read ahead too, then S
                     products<2 * KS, 4>([&](int i) { return i % 2 ? at.row(gt, 0, i / 2) : at.row(lds_address(vt), 32 * kw, i / 2); },
@@ -314,6 +328,7 @@ template <class T, int DP> __global__ __launch_bounds__(DP == 128 ? 512 : 256, 2
                                                   else p[y] = T::mma(x, k[ks], p[y]);
                                               });
                 }
+                __builtin_amdgcn_s_setprio(0);
 #pragma unroll
                 for (int y = 0; y < SUB; ++y)
 #pragma unroll
