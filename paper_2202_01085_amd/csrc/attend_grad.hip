@@ -444,22 +444,32 @@ template <class T> __global__ __launch_bounds__(NT) void join_keys(AttendArgs a)
     *(u32x2 *)(a.dv.p + 2 * (row * a.dv.row + (int64_t)hk * a.dv.head + x)) = (u32x2){T::pack(v.x, v.y), T::pack(v.z, v.w)};
 }
 
-// How grad_keys is cut.  A block has a CU to itself at head sizes above 64, half of one below: 256 or 512 at a time.  Key tiles whose
-// rows are more than an even share of the work are cut into parts of that size where there are too few tiles to even it out; with a
-// window all have about the same rows but those of the sinks, which all later tokens see.
+// How grad_keys is cut.  A block has a CU to itself at head sizes above 64, half of one below: 256 or 512 run at a time.  Key tiles are
+// cut into parts where there are too few of them to fill and even out the rounds: the number of parts that makes the shortest time
+// by counting row tiles, and `ends` of them for a block's beginning and end.  With a window all key tiles have about the same rows
+// (`usual`) but those of the sinks, which all later tokens see and which are always cut to the others' size.
 void cut_keys(AttendArgs &a, int64_t max_k) {
-    const int64_t tiles = cdiv(max_k, 128), items = tiles * a.groups, slots = a.dim > 64 ? 256 : 512;
+    const int64_t tiles = cdiv(max_k, 128), all = tiles * a.groups, slots = a.dim > 64 ? 256 : 512, ends = a.dim > 64 ? 12 : 4;
     const int64_t longest = std::max<int64_t>(1, cdiv(a.max_q, RT) * a.group);
-    int64_t usual = longest, work = items * longest / (a.causal ? 2 : 1);
-    if (a.window) usual = std::min(longest, (cdiv((int64_t)a.window + 128, RT) + 1) * a.group);
+    const int64_t usual = a.window ? std::min(longest, (cdiv((int64_t)a.window + 128, RT) + 1) * a.group) : longest;
     const int64_t sinks = usual < longest ? std::min(tiles, cdiv(a.sinks, 128)) : 0;
-    if (usual < longest) work = std::min(work, items * usual + sinks * a.groups * longest);
-    int64_t chunk = std::max<int64_t>(4, cdiv(work, slots));
-    const bool all = chunk < usual && items < 2 * slots;
-    if (!all) chunk = usual;
+    const bool even = usual < longest || !a.causal;      // else lengths fall to nothing along the keys
+    int64_t parts = 1;
+    double least = 1e30;
+    for (int64_t p = 1; p <= 64 && (p == 1 || all * p <= 4 * slots); ++p) {
+        const int64_t chunk = cdiv(usual, p), more = sinks * a.groups * std::max<int64_t>(0, cdiv(longest, chunk) - p);
+        const int64_t rounds = cdiv(all * p + more, slots);
+        const double cost = even ? (double)(rounds * (chunk + ends))
+                                 : std::max((double)chunk, (double)(all * usual) / (2.0 * (double)slots) + 0.5 * (double)chunk) + (double)(ends * rounds);
+        if (cost < least) {
+            least = cost;
+            parts = p;
+        }
+    }
+    const int64_t chunk = cdiv(usual, parts);
     a.tiles = (int)tiles;
     a.chunk = (int)chunk;
-    a.split = (int)(all ? tiles : sinks);
+    a.split = (int)(parts > 1 ? tiles : sinks);
     a.usual = (int)cdiv(usual, chunk);
     a.parts = (int)std::max<int64_t>(a.usual, a.split ? cdiv(longest, chunk) : 1);
     if (a.parts == 1) a.split = 0;
