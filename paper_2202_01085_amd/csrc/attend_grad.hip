@@ -19,30 +19,6 @@ constexpr int NT = 256;
 // log2 of the factor that grad_keys holds weights with
 template <class T> constexpr float LIFT = T::narrow ? 12.f : 0.f;
 
-// stat: -log2 of the row's sum (+ LIFT), or -inf for an empty row, so that its weights are 0, and -dO.O; 16 lanes to a row, 8 values each
-template <class T> __global__ __launch_bounds__(NT) void row_stats(AttendArgs a) {
-    const int64_t row = (int64_t)blockIdx.x * 16 + threadIdx.x / 16, all = a.total_q * a.heads;
-    const int x = threadIdx.x % 16 * 8;
-    float sum = 0.f;
-    const int64_t token = row / a.heads;
-    const int head = (int)(row % a.heads);
-    if (row < all && x < a.dim) {
-        const s16x8 g = *(const s16x8 *)(a.dout.p + 2 * (token * a.dout.row + (int64_t)head * a.dout.head + x));
-        const s16x8 o = *(const s16x8 *)(a.out.p + 2 * (token * a.out.row + (int64_t)head * a.out.head + x));
-#pragma unroll
-        for (int j = 0; j < 8; ++j) sum += T::up((uint16_t)g[j]) * T::up((uint16_t)o[j]);
-    }
-#pragma unroll
-    for (int by = 8; by > 0; by >>= 1) sum += __shfl_xor(sum, by);
-    if (row < all && x == 0) {
-        const float l = a.lse[row];
-        const bool empty = l == NO_KEY;
-        // a row whose dO or O is not finite makes what it adds to its keys NaN (also where tiles are cleaned)
-        a.stat[head * a.total_q + token] = empty ? NO_KEY : LIFT<T> - l * LOG2E + (sum - sum);
-        a.stat[(a.heads + head) * a.total_q + token] = empty ? 0.f : -sum;
-    }
-}
-
 // a power of two per lane that dS is divided by (fp16): raised, and what is summed so far lowered, when a larger dS comes
 struct Unit {
     float u;   // dS / u is at most 2^15
@@ -69,7 +45,8 @@ struct Unit {
 };
 constexpr float LEAST_UNIT = 0x1p-100f;
 
-// dQ: 128 rows of one group to a block, 32 to a wave, tiles of 64 keys through LDS, as the forward kernel
+// dQ: 128 rows of one group to a block, 32 to a wave, tiles of 64 keys through LDS, as the forward kernel.  It also leaves each row's
+// stat for grad_keys: -log2 of its sum (+ LIFT), or -inf for an empty row, so that its weights are 0, and -dO.O.
 template <class T, int DP> __global__ __launch_bounds__(NT, 2) void grad_rows(AttendArgs a) {
     constexpr int KS = DP / 16, DB = DP / 32, KT = 64;
     __shared__ __attribute__((aligned(1024))) short tile[2][2][KT * DP];
@@ -88,14 +65,34 @@ template <class T, int DP> __global__ __launch_bounds__(NT, 2) void grad_rows(At
     const Limits mine = limits_of(a, s, token);
     const Limits wfirst = limits_of(a, s, min(w0, rows - 1) / a.group), wlast = limits_of(a, s, min(w0 + 31, rows - 1) / a.group);
     const float c = a.scale * LOG2E;
-    const float less = a.stat[(int64_t)head * a.total_q + s.q0 + token] - LIFT<T>, delta = a.stat[(int64_t)(a.heads + head) * a.total_q + s.q0 + token];
-
     s16x8 q[KS], g[KS];
     f32x16 acc[DB];
 #pragma unroll
     for (int ks = 0; ks < KS; ++ks) {
         q[ks] = __builtin_bit_cast(s16x8, load_piece<DP>(a.q.p, (int64_t)(s.q0 + token) * a.q.row + (int64_t)head * a.q.head, 2 * ks + (lane >> 5), a.dim));
         g[ks] = __builtin_bit_cast(s16x8, load_piece<DP>(a.dout.p, (int64_t)(s.q0 + token) * a.dout.row + (int64_t)head * a.dout.head, 2 * ks + (lane >> 5), a.dim));
+    }
+    float less, delta = 0.f;
+    {
+        s16x8 o[KS];
+#pragma unroll
+        for (int ks = 0; ks < KS; ++ks)
+            o[ks] = __builtin_bit_cast(s16x8, load_piece<DP>(a.out.p, (int64_t)(s.q0 + token) * a.out.row + (int64_t)head * a.out.head, 2 * ks + (lane >> 5), a.dim));
+        const float l = a.lse[(int64_t)(s.q0 + token) * a.heads + head];
+#pragma unroll
+        for (int ks = 0; ks < KS; ++ks)
+#pragma unroll
+            for (int j = 0; j < 8; ++j) delta -= T::up((uint16_t)g[ks][j]) * T::up((uint16_t)o[ks][j]);
+        delta = both_halves_sum(delta);
+        const bool empty = l == NO_KEY;
+        // a row whose dO or O is not finite makes what it adds to its keys NaN (also where tiles are cleaned)
+        less = empty ? NO_KEY : -l * LOG2E + (delta - delta);
+        if (empty) delta = 0.f;
+        if (valid && lane < 32) {
+            const int64_t x = (int64_t)head * a.total_q + s.q0 + token;
+            a.stat[x] = less + LIFT<T>;
+            a.stat[x + (int64_t)a.heads * a.total_q] = delta;
+        }
     }
     Unit unit{LEAST_UNIT};
     LaneReads<DP> at;
@@ -485,8 +482,6 @@ int64_t stat_floats(const AttendArgs &a) { return cdiv(2 * a.total_q * a.heads, 
 
 template <class T, int DP> void launch(AttendArgs a, int64_t max_k, hipStream_t st) {
     if (a.max_q && a.total_q) {
-        row_stats<T><<<dim3((uint32_t)cdiv(a.total_q * a.heads, 16)), NT, 0, st>>>(a);
-        F3M_HIP(hipGetLastError());
         a.tiles = (int)cdiv((int64_t)a.max_q * a.group, 128);
         const int64_t blocks = attend_blocks(a, a.tiles);
         grad_rows<T, DP><<<dim3((uint32_t)blocks), NT, 0, st>>>(a);
