@@ -88,18 +88,17 @@ template <class T, int DP> __global__ __launch_bounds__(NT, 2) void grad_rows(At
         // a row whose dO or O is not finite makes what it adds to its keys NaN (also where tiles are cleaned)
         less = empty ? NO_KEY : -l * LOG2E + (delta - delta);
         if (empty) delta = 0.f;
-        if (valid && lane < 32) {
-            const int64_t x = (int64_t)head * a.total_q + s.q0 + token;
-            a.stat[x] = less + LIFT<T>;
-            a.stat[x + (int64_t)a.heads * a.total_q] = delta;
-        }
     }
     Unit unit{LEAST_UNIT};
     LaneReads<DP> at;
     at.start(lane);
-
-    auto block = [&](uint32_t kt, uint32_t vt, int kb, int key0, bool edge) {
-        f32x16 p = (f32x16)0.f, d = (f32x16)delta;     // dP starts from -dO.O
+    Tile2<T, DP, KT> src;
+    src.start(a.k.p + 2 * ((int64_t)s.k0 * a.k.row + (int64_t)hk * a.k.head), a.k.row, a.v.p + 2 * ((int64_t)s.k0 * a.v.row + (int64_t)hk * a.v.head), a.v.row, a.dim, wave, lane);
+    auto fetch = [&](int t, int buf) { src.issue(tiles[t] * KT, s.nk, a.dim, tile[buf][0], tile[buf][1], wave); };
+    // p = scores, d = dP - `from` of 32 keys of a tile
+    auto scores = [&](uint32_t kt, uint32_t vt, int kb, float from, f32x16 &p, f32x16 &d) {
+        p = (f32x16)0.f;
+        d = (f32x16)from;
         __builtin_amdgcn_s_setprio(1);      // the matrix cores to the wave that is at the scores, arithmetic to the other of the SIMD
         products<2 * KS, 4>([&](int i) { return at.row(i % 2 ? vt : kt, 32 * kb, i / 2); },
                             [&](int i, s16x8 x) {
@@ -107,6 +106,34 @@ template <class T, int DP> __global__ __launch_bounds__(NT, 2) void grad_rows(At
                                 else p = T::mma(x, q[i / 2], p);
                             });
         __builtin_amdgcn_s_setprio(0);
+    };
+
+    // Rows that see few keys have large results, whose rounding in dO.O would be as large an error as that of dS: where two tiles are all
+    // there is, dO.O is summed from the weights instead, sum_j P_ij dP_ij.
+    if (tiles.count > 0 && tiles.count <= 2) {
+        for (int n = 0; n < tiles.count; ++n) fetch(n, n);
+        registers_loaded();
+        __syncthreads();
+        float sum = 0.f;
+        for (int x = 0; x < 2 * tiles.count; ++x) {
+            f32x16 p, d;
+            scores(lds_address(tile[x / 2][0]), lds_address(tile[x / 2][1]), x % 2, 0.f, p, d);
+            const uint32_t bits = (uint32_t)seen_bits(mine, a.sinks, tiles[x / 2] * KT + 32 * (x % 2)) >> (4 * (lane >> 5));
+#pragma unroll
+            for (int i = 0; i < 16; ++i) sum += pick(bits, c_row(i, 0), __builtin_amdgcn_exp2f(__builtin_fmaf(p[i], c, less)) * d[i], 0.f);
+        }
+        delta = -both_halves_sum(sum);
+        __syncthreads();
+    }
+    if (valid && lane < 32) {
+        const int64_t x = (int64_t)head * a.total_q + s.q0 + token;
+        a.stat[x] = less + LIFT<T>;
+        a.stat[x + (int64_t)a.heads * a.total_q] = delta;
+    }
+
+    auto block = [&](uint32_t kt, uint32_t vt, int kb, int key0, bool edge) {
+        f32x16 p, d;
+        scores(kt, vt, kb, delta, p, d);     // dP starts from -dO.O
 #pragma unroll
         for (int i = 0; i < 16; ++i) d[i] = __builtin_amdgcn_exp2f(__builtin_fmaf(p[i], c, less)) * d[i];
         if (edge) {
@@ -126,9 +153,6 @@ template <class T, int DP> __global__ __launch_bounds__(NT, 2) void grad_rows(At
         for (int db = 0; db < DB; ++db) acc[db] = (f32x16)0.f;
         unit.u = LEAST_UNIT;
         if (tiles.count == 0) return;
-        Tile2<T, DP, KT> src;
-        src.start(a.k.p + 2 * ((int64_t)s.k0 * a.k.row + (int64_t)hk * a.k.head), a.k.row, a.v.p + 2 * ((int64_t)s.k0 * a.v.row + (int64_t)hk * a.v.head), a.v.row, a.dim, wave, lane);
-        auto fetch = [&](int t, int buf) { src.issue(tiles[t] * KT, s.nk, a.dim, tile[buf][0], tile[buf][1], wave); };
         // waits for the loads of tile t
         auto take = [&](int t, int buf) {
             arrived();
