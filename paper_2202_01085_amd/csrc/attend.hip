@@ -111,11 +111,15 @@ template <class T, int DP> struct Rows32 {
         spoil = 0.f;
     }
 
-    // NB blocks of 32 keys from key0 on: read_k(base, ks) is the A operand of k from row `base` on, v lies in LDS at vt.  edge: the mask cuts the tile for some row, or `good` (rows
-    // in pages of the cache) or `odd` (rows whose infinities or NaN in v are cleaned away) say something
-    template <int NB, class ReadK>
-    __device__ __forceinline__ void step(const LaneReads<DP> &at, ReadK &&read_k, uint32_t vt, int key0, bool edge, uint64_t good, uint64_t odd, const Limits &mine, int sinks,
-                                         float c, int lane) {
+    // NB blocks of 32 keys from key0 on: read_k(base, ks) is the A operand of k from row `base` on, v lies in LDS at vt, all of it or (half
+    // given) 16 rows at a time, which half(h) puts there.  edge: the mask cuts the tile for some row, or `good` (rows in pages of the cache) says
+    // something.  Returns the bits of the keys that the row sees.
+    struct Whole {};
+    template <int NB, class ReadK, class Half = Whole>
+    __device__ __forceinline__ uint64_t step(const LaneReads<DP> &at, ReadK &&read_k, uint32_t vt, int key0, bool edge, uint64_t good, const Limits &mine, int sinks,
+                                             float c, int lane, Half &&half = Whole{}) {
+        constexpr bool HALVES = !std::is_same<typename std::decay<Half>::type, Whole>::value;
+        uint64_t seen = ~0ull;
         f32x16 s[NB];
 #pragma unroll
         for (int kb = 0; kb < NB; ++kb) s[kb] = (f32x16)0.f;
@@ -124,8 +128,8 @@ template <class T, int DP> struct Rows32 {
         products<NB * KS, 4>([&](int i) { return read_k(32 * (i % NB), i / NB); }, [&](int i, s16x8 x) { s[i % NB] = T::mma(x, q[i / NB], s[i % NB]); });
         __builtin_amdgcn_s_setprio(0);
         if (edge) {
-            const uint64_t seen = seen_bits(mine, sinks, key0) & good, bits = seen >> (4 * (lane >> 5));
-            if (seen & odd) spoil = __builtin_nanf("");
+            seen = seen_bits(mine, sinks, key0) & good;
+            const uint64_t bits = seen >> (4 * (lane >> 5));
 #pragma unroll
             for (int kb = 0; kb < NB; ++kb)
 #pragma unroll
@@ -160,6 +164,14 @@ template <class T, int DP> struct Rows32 {
 #pragma unroll
         for (int kb = 0; kb < NB; ++kb) {
             const s16x8 w[2] = {as_operand<T>(s[kb], 0), as_operand<T>(s[kb], 1)};
+            if constexpr (HALVES) {
+#pragma unroll
+                for (int h = 0; h < 2; ++h) {
+                    half(h);
+                    products<DB, 2>([&](int i) { return at.column(vt, 0, i); }, [&](int i, s16x8 x) { o[i] = T::mma(x, w[h], o[i]); });
+                }
+                continue;
+            }
             // the exponentials of the next block run under the products of this one
             products<2 * DB, 2>([&](int i) { return at.column(vt, 32 * kb + 16 * (i / DB), i % DB); },
                                 [&](int i, s16x8 x) {
@@ -167,6 +179,7 @@ template <class T, int DP> struct Rows32 {
                                     if (kb + 1 < NB) weigh(kb + 1 < NB ? kb + 1 : 0, 16 * i / (2 * DB), 16 * (i + 1) / (2 * DB));
                                 });
         }
+        return seen;
     }
     __device__ bool finite() const {
         bool all = true;
@@ -253,7 +266,9 @@ template <class T, int DP, bool E8> __global__ __launch_bounds__(NT, DP == 128 ?
             const bool none = idle || key0 >= wlast.hi || (key0 + KT <= wfirst.lo && key0 >= a.sinks);
             const bool full = key0 + KT <= wfirst.hi && (key0 >= wlast.lo || key0 + KT <= a.sinks) && ok == ~0ull && odd == 0;
             const uint32_t kt = lds_address(tile[buf][0]);
-            if (!none) r.template step<2>(at, [&](int base, int ks) { return at.row(kt, base, ks); }, lds_address(tile[buf][1]), key0, !full, ok, odd, mine, a.sinks, c, lane);
+            if (none) return;
+            const uint64_t seen = r.template step<2>(at, [&](int base, int ks) { return at.row(kt, base, ks); }, lds_address(tile[buf][1]), key0, !full, ok, mine, a.sinks, c, lane);
+            if (seen & odd) r.spoil = __builtin_nanf("");
         };
         if (n >= end) return;
         if constexpr (E8) {
@@ -337,11 +352,10 @@ template <class T, int DP, bool E8> __global__ __launch_bounds__(NT, DP == 128 ?
 // tile of 32 keys through a ring in LDS of its own, and the four results are joined at the end.  Bound by the reading of K and V.
 constexpr int PAGES_MAX = 1024;   // page numbers of a work item
 
-template <class T, int DP, bool E8> __global__ __launch_bounds__(NT, 1) void attend_few(AttendArgs a) {
+template <class T, int DP, bool E8> __global__ __launch_bounds__(NT, E8 ? 2 : 1) void attend_few(AttendArgs a) {
     using Row = Rows32<T, DP>;
     constexpr int N = 32, BYTES = E8 ? 1 : 2, PIECES = DP * BYTES / 16, RPI = 64 / PIECES, COUNT = N / RPI;   // pieces of a row, rows to an instruction
-    constexpr int RING = E8 ? 3 : 2, TILE = N * DP * BYTES, SLOT = 2 * TILE + (E8 ? 256 : 0), LOADS = 2 * COUNT + (E8 ? 1 : 0);
-    constexpr int OF_WAVE = RING * SLOT + (E8 ? 2 * N * DP : 0);                                           // 8 bits: and a tile of v as 16-bit values
+    constexpr int RING = 2, TILE = N * DP * BYTES, SLOT = 2 * TILE + (E8 ? 256 : 0), LOADS = 2 * COUNT + (E8 ? 1 : 0), OF_WAVE = RING * SLOT;
     __shared__ __attribute__((aligned(1024))) char lds[4 * OF_WAVE];
     __shared__ int pages[PAGES_MAX];
     __shared__ float joined[4][2][32];
@@ -382,7 +396,7 @@ template <class T, int DP, bool E8> __global__ __launch_bounds__(NT, 1) void att
 
     // the exchange of 16-byte pieces of a tile of codes: rows of one piece spread over all banks
     auto swap = [](int x) { return E8 ? (DP == 128 ? (x >> 1) & 7 : DP == 64 ? (x >> 2) & 3 : (x >> 3) & 1) : piece_swap<DP>(x); };
-    const uint32_t ring = lds_address((const short *)lds) + wave * OF_WAVE, v16 = ring + RING * SLOT;
+    const uint32_t ring = lds_address((const short *)lds) + wave * OF_WAVE;
     auto fetch = [&](int n, int slot) {
         const int key0 = tiles[n] * N;
         const uint32_t to = ring + slot * SLOT;
@@ -417,43 +431,8 @@ template <class T, int DP, bool E8> __global__ __launch_bounds__(NT, 1) void att
             if (a.table) good = __ballot(pages[(n - begin) * subs + ((lane & 31) >> shift)] >= 0);
             const bool whole = key0 + N <= first.hi && (key0 >= last.lo || key0 + N <= a.sinks) && good == ~0ull;
             arrived<(RING - 1) * LOADS>();
-            uint64_t odd = 0;
+            uint64_t odd = 0, seen;
             using lds_piece = __attribute__((address_space(3))) u32x4;
-            if constexpr (E8) {
-                // v as 16-bit values, for transposing reads; k is converted as it is read
-                using lds_byte = __attribute__((address_space(3))) const uint8_t;
-#pragma unroll
-                for (int x = 0; x < COUNT; ++x) {
-                    const int in = x * RPI + lane / PIECES, piece = (lane % PIECES) ^ swap(in);
-                    const u32x4 w = *(lds_piece *)(uintptr_t)(vt + 1024 * x + 16 * lane);
-                    const float scale = __builtin_bit_cast(float, (uint32_t)*(lds_byte *)(uintptr_t)(kt + 2 * TILE + 32 + in) << 23);
-#pragma unroll
-                    for (int h = 0; h < 2; ++h) {
-                        u32x4 y = {T::template codes<false>(w[2 * h], scale), T::template codes<true>(w[2 * h], scale),
-                                   T::template codes<false>(w[2 * h + 1], scale), T::template codes<true>(w[2 * h + 1], scale)};
-                        if (!whole && any_odd<T>(y)) {
-                            y = cleaned<T>(y);
-                            odd |= 1ull << in;
-                        }
-                        *(lds_piece *)(uintptr_t)(v16 + 2 * tile_at<DP>(in, 2 * piece + h)) = y;
-                    }
-                }
-            } else if (!whole) {
-#pragma unroll 2
-                for (int x = 0; x < COUNT; ++x) {
-                    lds_piece *const p = (lds_piece *)(uintptr_t)(vt + 1024 * x + 16 * lane);
-                    const u32x4 w = *p;
-                    if (any_odd<T>(w)) {
-                        *p = cleaned<T>(w);
-                        odd |= 1ull << (x * RPI + lane / PIECES);
-                    }
-                }
-            }
-            if (!whole && __any(odd != 0)) {
-#pragma unroll 1
-                for (int by = 32; by > 0; by >>= 1) odd |= __shfl_xor((unsigned long long)odd, by);
-            }
-            __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");   // LDS does a wave's accesses in their order: nothing to wait for
             if constexpr (E8) {
                 using lds_byte = __attribute__((address_space(3))) const uint8_t;
                 using lds_codes = __attribute__((address_space(3))) const u32x2;
@@ -464,9 +443,48 @@ template <class T, int DP, bool E8> __global__ __launch_bounds__(NT, 1) void att
                     return __builtin_bit_cast(s16x8, (u32x4){T::template codes<false>(w[0], scale), T::template codes<true>(w[0], scale),
                                                             T::template codes<false>(w[1], scale), T::template codes<true>(w[1], scale)});
                 };
-                r.template step<1>(at, read_k, v16, key0, !whole, good, odd, mine, a.sinks, c, lane);
+                // 16 rows of v as 16-bit values, for transposing reads, where k was: k is not needed any more
+                auto half = [&](int h) {
+                    __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");   // LDS does a wave's accesses in their order: nothing to wait for
+#pragma unroll
+                    for (int x = 0; x < COUNT; ++x) {
+                        const int in = x * RPI + lane / PIECES, piece = (lane % PIECES) ^ swap(in);
+                        if (COUNT > 1 ? x * RPI / 16 != h : in / 16 != h) continue;
+                        const u32x4 w = *(lds_piece *)(uintptr_t)(vt + 1024 * x + 16 * lane);
+                        const float by = __builtin_bit_cast(float, (uint32_t)*(lds_byte *)(uintptr_t)(kt + 2 * TILE + 32 + in) << 23);
+#pragma unroll
+                        for (int z = 0; z < 2; ++z) {
+                            u32x4 y = {T::template codes<false>(w[2 * z], by), T::template codes<true>(w[2 * z], by),
+                                       T::template codes<false>(w[2 * z + 1], by), T::template codes<true>(w[2 * z + 1], by)};
+                            if (!whole && any_odd<T>(y)) {
+                                y = cleaned<T>(y);
+                                odd |= 1ull << in;
+                            }
+                            *(lds_piece *)(uintptr_t)(kt + 2 * tile_at<DP>(in & 15, 2 * piece + z)) = y;
+                        }
+                    }
+                    __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");
+                };
+                seen = r.template step<1>(at, read_k, kt, key0, !whole, good, mine, a.sinks, c, lane, half);
             } else {
-                r.template step<1>(at, [&](int base, int ks) { return at.row(kt, base, ks); }, vt, key0, !whole, good, odd, mine, a.sinks, c, lane);
+                if (!whole) {
+#pragma unroll 2
+                    for (int x = 0; x < COUNT; ++x) {
+                        lds_piece *const p = (lds_piece *)(uintptr_t)(vt + 1024 * x + 16 * lane);
+                        const u32x4 w = *p;
+                        if (any_odd<T>(w)) {
+                            *p = cleaned<T>(w);
+                            odd |= 1ull << (x * RPI + lane / PIECES);
+                        }
+                    }
+                }
+                __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");
+                seen = r.template step<1>(at, [&](int base, int ks) { return at.row(kt, base, ks); }, vt, key0, !whole, good, mine, a.sinks, c, lane);
+            }
+            if (!whole && __any(odd != 0)) {
+#pragma unroll 1
+                for (int by = 32; by > 0; by >>= 1) odd |= __shfl_xor((unsigned long long)odd, by);
+                if (seen & odd) r.spoil = __builtin_nanf("");
             }
             __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");
             fetch(min(n + 4 * RING, final), slot);
