@@ -657,15 +657,16 @@ template <class T> void launch_dim(const AttendArgs &a, bool e8, bool few, int64
 }
 
 // Up to 64 rows to a key head go to attend_few.  A long key axis is cut into parts where the rows alone make too few blocks: two
-// blocks of attend_many fit a CU (three up to a head size of 64), one of attend_few, whose waves keep 64 KB or more under way.
-bool split(AttendArgs &a, int64_t max_k) {
+// blocks of attend_many fit a CU (three up to a head size of 64), one of attend_few (two with 8-bit codes), whose waves keep 64 KB or more
+// under way.
+bool split(AttendArgs &a, int64_t max_k, bool e8) {
     const bool few = (int64_t)a.max_q * a.group <= 64;
     const int per = few ? 32 : KT, rows = few ? 32 : 128, least = few ? 16 : 8;
     a.tiles = (int)cdiv((int64_t)a.max_q * a.group, rows);
     const int64_t most = most_tiles(a, max_k, rows, per), items = (int64_t)a.tiles * a.groups;
     int64_t parts = 1;
     if (few) {
-        parts = cdiv(1024, items);
+        parts = cdiv(e8 ? 2048 : 1024, items);   // four rounds, for sequences of different lengths
     } else if (const int64_t slots = a.dim > 64 ? 512 : 768; items < slots) {   // the fewest rounds of blocks for the work of one, a part costing some of it
         double least_cost = 1e30;
         for (int64_t p = 1; p <= slots; ++p) {
@@ -686,13 +687,17 @@ bool split(AttendArgs &a, int64_t max_k) {
 
 int64_t attend_workspace(AttendArgs a, int64_t max_k) {
     if (!a.max_q || !a.total_q || !a.groups) return 0;
-    split(a, max_k);
-    return a.parts > 1 ? (int64_t)a.parts * a.total_q * a.heads * (a.dim + 1) * (int64_t)sizeof(float) : 0;
+    int64_t parts = 1;           // of either kind of cache: the caller does not say
+    for (const bool e8 : {false, true}) {
+        split(a, max_k, e8);
+        parts = std::max<int64_t>(parts, a.parts);
+    }
+    return parts > 1 ? parts * a.total_q * a.heads * (a.dim + 1) * (int64_t)sizeof(float) : 0;
 }
 
 void run_attend(AttendArgs a, int64_t max_k, bool f16, bool e8, void *workspace, hipStream_t st) {
     if (!a.max_q || !a.total_q || !a.groups) return;
-    const bool few = split(a, max_k);
+    const bool few = split(a, max_k, e8);
     a.part_out = (float *)workspace;
     a.part_lse = a.part_out ? a.part_out + (int64_t)a.parts * a.total_q * a.heads * a.dim : nullptr;
     const int64_t blocks = attend_blocks(a, (int64_t)a.tiles * a.parts);
