@@ -267,28 +267,6 @@ __device__ __forceinline__ Item block_of(const AttendArgs &a, uint32_t at) {
     return w;
 }
 
-// ---- where the rows of K and V lie ----
-// Offset in values of row j of the sequence for key head hk, or in exponent bytes.  A page outside the cache is not touched: `ok`
-// comes back false and the offset is that of page 0.
-struct Place {
-    int64_t at, exp_at;
-    bool ok;
-};
-__device__ __forceinline__ Place place_of(const AttendArgs &a, const Sequence &s, int b, int hk, int j, const Rows &x) {
-    Place p;
-    if (!a.table) {
-        p.at = (int64_t)(s.k0 + j) * x.row + (int64_t)hk * x.head;
-        p.exp_at = 0;
-        p.ok = true;
-        return p;
-    }
-    const int page = a.table[(int64_t)b * a.table_row + (j >> a.page_shift)];
-    p.ok = page >= 0 && page < a.pages;
-    p.exp_at = (((int64_t)(p.ok ? page : 0) * a.kv_heads + hk) << a.page_shift) + (j & ((1 << a.page_shift) - 1));
-    p.at = p.exp_at * a.dim;
-    return p;
-}
-
 // ---- tiles straight from memory to LDS ----
 // 16 bytes to a lane, 1 KB to an instruction, in the order of LDS: lane i's bytes go to `lds` + 16 i.  So which piece of which row a lane
 // reads follows from where it has to lie (tile_at).  Written out, because the compiler, which cannot tell the tiles apart, would wait

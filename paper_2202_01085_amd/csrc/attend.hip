@@ -17,53 +17,49 @@ constexpr int NT = 256;       // four waves
 constexpr int KT = 64;        // keys of a tile
 constexpr float GROW = 8.f;   // log2 of how far a score may lie above m
 
-// Pieces of a tile of K and V on their way from memory to LDS, N rows for THREADS threads
-template <class T, int DP, bool E8, int N, int THREADS> struct Stage {
-    static constexpr int VALUES = E8 ? 16 : 8, PIECES = DP / VALUES, COUNT = (N * PIECES + THREADS - 1) / THREADS;
-    static constexpr bool ALL = N * PIECES % THREADS == 0;
+// A tile of K and V from an 8-bit cache on its way from memory to LDS, where it lies as 16-bit values: 16 codes to a thread's piece.  Page
+// numbers are looked up a tile before.
+template <class T, int DP> struct Codes {
+    static constexpr int PIECES = DP / 16, COUNT = (KT * PIECES + NT - 1) / NT;
+    static constexpr bool ALL = KT * PIECES % NT == 0;
     u32x4 k[COUNT], v[COUNT];
     uint8_t ke[COUNT], ve[COUNT];
+    int pages[COUNT], all;         // of the thread's rows; of row `lane` of the tile
 
-    __device__ void load(const AttendArgs &a, const Sequence &s, int b, int hk, int key0, int tid) {
+    __device__ void look(const AttendArgs &a, const Sequence &s, int b, int key0, int tid) {
+        const int *const table = a.table + (int64_t)b * a.table_row;
+#pragma unroll
+        for (int c = 0; c < COUNT; ++c) pages[c] = table[min(key0 + (tid + NT * c) / PIECES % KT, s.nk - 1) >> a.page_shift];
+        all = table[min(key0 + (tid & 63), s.nk - 1) >> a.page_shift];
+    }
+    // bits of the rows that lie in pages of the cache
+    __device__ uint64_t good(const AttendArgs &a) const { return __ballot(all >= 0 && all < a.pages); }
+    __device__ void load(const AttendArgs &a, const Sequence &s, int hk, int key0, int tid) {
 #pragma unroll
         for (int c = 0; c < COUNT; ++c) {
-            const int at = tid + THREADS * c, row = at / PIECES, piece = at % PIECES;
-            if (!ALL && row >= N) break;
-            const int j = min(key0 + row, s.nk - 1);
-            const Place p = place_of(a, s, b, hk, j, a.k);
-            const int64_t vat = a.table ? p.at : (int64_t)(s.k0 + j) * a.v.row + (int64_t)hk * a.v.head;
-            if (E8) {
-                const bool in = piece * 16 < a.dim;
-                k[c] = in ? *(const u32x4 *)(a.k.p + p.at + piece * 16) : (u32x4){0, 0, 0, 0};
-                v[c] = in ? *(const u32x4 *)(a.v.p + p.at + piece * 16) : (u32x4){0, 0, 0, 0};
-                ke[c] = a.k_exp[p.exp_at];
-                ve[c] = a.v_exp[p.exp_at];
-            } else {
-                k[c] = load_piece<DP>(a.k.p, p.at, piece, a.dim);
-                v[c] = load_piece<DP>(a.v.p, vat, piece, a.dim);
-            }
+            const int at = tid + NT * c, row = at / PIECES, piece = at % PIECES;
+            if (!ALL && row >= KT) break;
+            const int j = min(key0 + row, s.nk - 1), page = pages[c] >= 0 && pages[c] < a.pages ? pages[c] : 0;
+            const uint64_t x = (uint64_t)(uint32_t)page * (uint32_t)(a.kv_heads << a.page_shift) + (uint32_t)((hk << a.page_shift) + (j & ((1 << a.page_shift) - 1)));
+            const uint64_t y = x * (uint32_t)a.dim + (piece * 16 < a.dim ? piece * 16 : 0);   // past the head: q is 0 there, and o is not kept
+            k[c] = *(const u32x4 *)(a.k.p + y);
+            v[c] = *(const u32x4 *)(a.v.p + y);
+            ke[c] = a.k_exp[x];
+            ve[c] = a.v_exp[x];
         }
     }
     static __device__ bool put(short *tile, int row, int piece, u32x4 x, uint8_t e, bool clean) {
+        const float scale = __builtin_bit_cast(float, (uint32_t)e << 23);
         bool odd = false;
-        if (E8) {
-            const float scale = __builtin_bit_cast(float, (uint32_t)e << 23);
 #pragma unroll
-            for (int h = 0; h < 2; ++h) {
-                u32x4 w = {T::template codes<false>(x[2 * h], scale), T::template codes<true>(x[2 * h], scale),
-                           T::template codes<false>(x[2 * h + 1], scale), T::template codes<true>(x[2 * h + 1], scale)};
-                if (clean && any_odd<T>(w)) {
-                    w = cleaned<T>(w);
-                    odd = true;
-                }
-                *(u32x4 *)(tile + tile_at<DP>(row, 2 * piece + h)) = w;
-            }
-        } else {
-            if (clean && any_odd<T>(x)) {
-                x = cleaned<T>(x);
+        for (int h = 0; h < 2; ++h) {
+            u32x4 w = {T::template codes<false>(x[2 * h], scale), T::template codes<true>(x[2 * h], scale),
+                       T::template codes<false>(x[2 * h + 1], scale), T::template codes<true>(x[2 * h + 1], scale)};
+            if (clean && any_odd<T>(w)) {
+                w = cleaned<T>(w);
                 odd = true;
             }
-            *(u32x4 *)(tile + tile_at<DP>(row, piece)) = x;
+            *(u32x4 *)(tile + tile_at<DP>(row, 2 * piece + h)) = w;
         }
         return odd;
     }
@@ -72,8 +68,8 @@ template <class T, int DP, bool E8, int N, int THREADS> struct Stage {
         uint64_t odd = 0;
 #pragma unroll
         for (int c = 0; c < COUNT; ++c) {
-            const int at = tid + THREADS * c, row = at / PIECES, piece = at % PIECES;
-            if (!ALL && row >= N) break;
+            const int at = tid + NT * c, row = at / PIECES, piece = at % PIECES;
+            if (!ALL && row >= KT) break;
             put(kt, row, piece, k[c], ke[c], false);
             if (put(vt, row, piece, v[c], ve[c], clean)) odd |= 1ull << row;
         }
@@ -272,17 +268,19 @@ template <class T, int DP, bool E8> __global__ __launch_bounds__(NT, DP == 128 ?
         };
         if (n >= end) return;
         if constexpr (E8) {
-            Stage<T, DP, E8, KT, NT> next;
+            Codes<T, DP> next;
             uint64_t good = 0;
-            auto fetch = [&](int t) {
-                next.load(a, s, b, hk, tiles[t] * KT, tid);
-                if (wave == 0) good = good_pages(a, s, b, tiles[t] * KT, lane);
+            auto fetch = [&](int t) {             // its pages are looked up; those of the tile after it follow
+                next.load(a, s, hk, tiles[t] * KT, tid);
+                good = next.good(a);
+                if (t + 1 < end) next.look(a, s, b, tiles[t + 1] * KT, tid);
             };
             auto keep = [&](int t, int buf) {
                 const uint64_t odd = next.store(tile[buf][0], tile[buf][1], tid, careful && !whole(tiles[t] * KT));
                 if (careful && lane == 0) odd_rows[buf][wave] = odd;
                 if (tid == 0) good_rows[buf] = good;
             };
+            next.look(a, s, b, tiles[n] * KT, tid);
             fetch(n);
             keep(n, n & 1);
             registers_loaded();
