@@ -96,11 +96,11 @@ void run_attend_grad(AttendArgs a, int64_t max_k, bool f16, void *workspace, hip
 void run_cache_rows(const f3m_cache &c, bool f16, const int64_t *slot, int64_t tokens, const f3m_rows &k, const f3m_rows &v, bool write,
                     hipStream_t st);
 
-// ---- tiles in LDS: rows of DP values, their 16-byte pieces exchanged so that neither 8 rows read at one piece (row) nor
-// 4 rows read at two neighbouring ones (column) meet in a bank ----
+// ---- tiles in LDS: rows of DP values, their 16-byte pieces exchanged so that what a read takes at once lies in different banks: 16 rows at
+// one piece (row), four rows at four neighbouring pieces (column) ----
 template <int DP> __device__ __forceinline__ int piece_swap(int r) {
-    if (DP == 128) return ((r & 7) << 1) ^ ((r >> 3) & 1);
-    if (DP == 64) return (r & 6) ^ ((r >> 3) & 1);
+    if (DP == 128) return ((r & 3) << 2) | ((r >> 2) & 3);
+    if (DP == 64) return ((r & 2) << 1) | ((r >> 2) & 3);
     return (r >> 2) & 3;   // 32
 }
 template <int DP> __device__ __forceinline__ int tile_at(int r, int piece) {   // in values
@@ -127,7 +127,7 @@ template <int DP> struct LaneReads {
     // A operand whose rows are dimensions 32 db .. 32 db + 31 and whose summands are rows base .. base + 15 (base a multiple of 16) of the
     // tile, in the order above: four rows to a read, transposed on the way
     __device__ s16x8 column(uint32_t tile, int base, int db) const {
-        constexpr uint32_t EIGHT = DP == 32 ? 32 : 16;   // what the exchange of a row 8 further adds
+        constexpr uint32_t EIGHT = 32;   // what the exchange of a row 8 further adds
         const s16x4 x = __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds_s16x4 *)(uintptr_t)(((tile + t) ^ (64 * db)) + 2 * DP * base));
         const s16x4 y = __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds_s16x4 *)(uintptr_t)(((tile + t) ^ (64 * db) ^ EIGHT) + 2 * DP * (base + 8)));
         return __builtin_shufflevector(x, y, 0, 1, 2, 3, 4, 5, 6, 7);
