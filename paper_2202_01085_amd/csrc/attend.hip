@@ -667,7 +667,8 @@ bool split(AttendArgs &a, int64_t max_k, bool e8) {
         parts = cdiv(e8 ? 2048 : 1024, items);   // four rounds, for sequences of different lengths
     } else if (const int64_t slots = a.dim > 64 ? 512 : 768; items < slots) {   // the fewest rounds of blocks for the work of one, a part costing some of it
         double least_cost = 1e30;
-        for (int64_t p = 1; p <= slots; ++p) {
+        for (int64_t rounds = 0; rounds <= 6; ++rounds) {   // as many parts as fill them; 0: one part
+            const int64_t p = rounds ? rounds * slots / items : 1;
             const double cost = (double)cdiv(items * p, slots) / (double)p + 0.02 * (double)p * (double)items / (double)slots;
             if (cost < least_cost) {
                 least_cost = cost;

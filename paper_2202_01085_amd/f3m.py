@@ -457,9 +457,9 @@ def _packed_args(q, k, v, q_offsets, k_offsets, max_q, max_k, scale, causal, win
     return _attention_args(q, shape, rq, rk, rv, heads, rows, q_offsets, k_offsets, max_q, max_k, scale, causal, window, sinks)
 
 
-def _lse(lse, shape, device):
+def _lse(lse, shape, device, q=None):
     if lse is None:
-        return torch.empty(shape, dtype=torch.float32, device=device)
+        return q.new_empty(shape, dtype=torch.float32)
     _device_array(lse, "lse", torch.float32, device, shape)
     return lse
 
@@ -487,9 +487,9 @@ def attention(q, k, v, q_offsets=None, k_offsets=None, max_q=None, max_k=None, s
     device, shape = q.device, q.shape
 
     def call(handle):
-        o = torch.empty(shape, dtype=q.dtype, device=device) if out is None else out
+        o = torch.empty_like(q) if out is None else out
         to = _rows(o, "out", q.dtype, device, shape)
-        ls = _lse(lse, shape[:2], device)
+        ls = _lse(lse, shape[:2], device, q)
         L = lib()
         w, at, need = _workspace(L.f3m_attention_workspace, a, device)
         _check(L.f3m_attention(ctypes.byref(a), ctypes.byref(to), ls.data_ptr() or None, at, need, handle))
@@ -509,7 +509,7 @@ def attention_grad(dout, q, k, v, out, lse, q_offsets=None, k_offsets=None, max_
     _lse(lse, shape[:2], device)
 
     def call(handle):
-        got = [torch.empty(x.shape, dtype=dtype, device=device) if y is None else y for x, y in ((q, dq), (k, dk), (v, dv))]
+        got = [torch.empty_like(x) if y is None else y for x, y in ((q, dq), (k, dk), (v, dv))]
         to = [_rows(y, name, dtype, device, x.shape) for y, name, x in zip(got, ("dq", "dk", "dv"), (q, k, v))]
         L = lib()
         w, at, need = _workspace(L.f3m_attention_grad_workspace, a, device)
@@ -571,8 +571,8 @@ class KVCache:
         shape = (slots.numel(), self._c.kv_heads, self._c.head_dim)
 
         def call(handle):
-            kk = torch.empty(shape, dtype=dtype, device=self.k.device) if k is None else k
-            vv = torch.empty(shape, dtype=dtype, device=self.k.device) if v is None else v
+            kk = slots.new_empty(shape, dtype=dtype) if k is None else k
+            vv = slots.new_empty(shape, dtype=dtype) if v is None else v
             self._move(lib().f3m_cache_read, kk, vv, slots, handle)
             return kk, vv
 
@@ -611,9 +611,9 @@ class KVCache:
                                 scale, causal, window, sinks)
             if a.batch != batch:
                 raise ValueError("q_offsets must have one entry more than the table has rows")
-            o = torch.empty(shape, dtype=q.dtype, device=device) if out is None else out
+            o = torch.empty_like(q) if out is None else out
             to = _rows(o, "out", q.dtype, device, shape)
-            ls = _lse(lse, shape[:2], device)
+            ls = _lse(lse, shape[:2], device, q)
             L = lib()
             w, at, need = _workspace(L.f3m_attention_workspace, a, device)
             _check(L.f3m_cache_attention(ctypes.byref(c), ctypes.byref(a), table.data_ptr() or None, max(step, cols), cols, ln, ctypes.byref(to),
