@@ -65,14 +65,6 @@ template <class T, int DP> __global__ __launch_bounds__(NT, 2) void grad_rows(At
     const Limits mine = limits_of(a, s, token);
     const Limits wfirst = limits_of(a, s, min(w0, rows - 1) / a.group), wlast = limits_of(a, s, min(w0 + 31, rows - 1) / a.group);
     const float c = a.scale * LOG2E;
-    Tile2<T, DP, KT> src;
-    src.start(a.k.p + 2 * ((int64_t)s.k0 * a.k.row + (int64_t)hk * a.k.head), a.k.row, a.v.p + 2 * ((int64_t)s.k0 * a.v.row + (int64_t)hk * a.v.head), a.v.row, a.dim, wave, lane);
-    auto fetch = [&](int t, int buf) { src.issue(tiles[t] * KT, s.nk, a.dim, tile[buf][0], tile[buf][1], wave); };
-    // the first tile is on its way before the rows are read, the second too if there is no third: both then stay
-    const bool all_there = tiles.count <= 2;
-    if (tiles.count > 0) fetch(0, 0);
-    if (tiles.count == 2) fetch(1, 1);
-
     s16x8 q[KS], g[KS];
     f32x16 acc[DB];
 #pragma unroll
@@ -100,6 +92,9 @@ template <class T, int DP> __global__ __launch_bounds__(NT, 2) void grad_rows(At
     Unit unit{LEAST_UNIT};
     LaneReads<DP> at;
     at.start(lane);
+    Tile2<T, DP, KT> src;
+    src.start(a.k.p + 2 * ((int64_t)s.k0 * a.k.row + (int64_t)hk * a.k.head), a.k.row, a.v.p + 2 * ((int64_t)s.k0 * a.v.row + (int64_t)hk * a.v.head), a.v.row, a.dim, wave, lane);
+    auto fetch = [&](int t, int buf) { src.issue(tiles[t] * KT, s.nk, a.dim, tile[buf][0], tile[buf][1], wave); };
     // p = scores, d = dP - `from` of 32 keys of a tile
     auto scores = [&](uint32_t kt, uint32_t vt, int kb, float from, f32x16 &p, f32x16 &d) {
         p = (f32x16)0.f;
@@ -115,7 +110,8 @@ template <class T, int DP> __global__ __launch_bounds__(NT, 2) void grad_rows(At
 
     // Rows that see few keys have large results, whose rounding in dO.O would be as large an error as that of dS: where two tiles are all
     // there is, dO.O is summed from the weights instead, sum_j P_ij dP_ij.
-    if (tiles.count > 0 && all_there) {
+    if (tiles.count > 0 && tiles.count <= 2) {
+        for (int n = 0; n < tiles.count; ++n) fetch(n, n);
         registers_loaded();
         __syncthreads();
         float sum = 0.f;
@@ -127,6 +123,7 @@ template <class T, int DP> __global__ __launch_bounds__(NT, 2) void grad_rows(At
             for (int i = 0; i < 16; ++i) sum += pick(bits, c_row(i, 0), __builtin_amdgcn_exp2f(__builtin_fmaf(p[i], c, less)) * d[i], 0.f);
         }
         delta = -both_halves_sum(sum);
+        __syncthreads();
     }
     if (valid && lane < 32) {
         const int64_t x = (int64_t)head * a.total_q + s.q0 + token;
@@ -165,20 +162,19 @@ template <class T, int DP> __global__ __launch_bounds__(NT, 2) void grad_rows(At
             clean_tile<T, DP, KT>(tile[buf][0], tid);
             __syncthreads();
         };
-        const bool load = careful || !all_there;      // the first pass finds the first tile on its way, or all there
-        if (careful) fetch(0, 0);
+        fetch(0, 0);
         registers_loaded();
-        if (load) take(0, 0);
+        take(0, 0);
         for (int n = 0; n < tiles.count; ++n) {
             const int buf = n & 1, key0 = tiles[n] * KT;
-            if (load && n + 1 < tiles.count) fetch(n + 1, buf ^ 1);
+            if (n + 1 < tiles.count) fetch(n + 1, buf ^ 1);
             const bool none = idle || key0 >= wlast.hi || (key0 + KT <= wfirst.lo && key0 >= a.sinks);
             const bool full = key0 + KT <= wfirst.hi && (key0 >= wlast.lo || key0 + KT <= a.sinks);
             if (!none) {
                 block(lds_address(tile[buf][0]), lds_address(tile[buf][1]), 0, key0, !full);
                 block(lds_address(tile[buf][0]), lds_address(tile[buf][1]), 1, key0, !full);
             }
-            if (load && n + 1 < tiles.count) take(n + 1, buf ^ 1);
+            if (n + 1 < tiles.count) take(n + 1, buf ^ 1);
         }
     };
     pass(false);
@@ -262,6 +258,24 @@ template <class T, int DP> __global__ __launch_bounds__(DP == 128 ? 512 : 256, 2
     const int2 all_block = seen_by_all(k0, k0 + 128), all_wave = seen_by_all(w0, w0 + 32);
     const float c = a.scale * LOG2E;
 
+    s16x8 k[KS], v[V_LDS ? 1 : KS];
+    f32x16 dk[DB], dv[DB];
+#pragma unroll
+    for (int ks = 0; ks < KS; ++ks) {
+        k[ks] = __builtin_bit_cast(s16x8, load_piece<DP>(a.k.p, (int64_t)(s.k0 + kept) * a.k.row + (int64_t)hk * a.k.head, 2 * ks + (lane >> 5), a.dim));
+        if (!V_LDS) v[V_LDS ? 0 : ks] = __builtin_bit_cast(s16x8, load_piece<DP>(a.v.p, (int64_t)(s.k0 + kept) * a.v.row + (int64_t)hk * a.v.head, 2 * ks + (lane >> 5), a.dim));
+    }
+    if (V_LDS)
+        for (int at = tid; at < 128 * (DP / 8); at += THREADS) {
+            const int r = at / (DP / 8), piece = at % (DP / 8);
+            *(u32x4 *)(vt + tile_at<DP>(r, piece)) = load_piece<DP>(a.v.p, (int64_t)(s.k0 + min(k0 + r, s.nk - 1)) * a.v.row + (int64_t)hk * a.v.head, piece, a.dim);
+        }
+#pragma unroll
+    for (int db = 0; db < DB; ++db) { dk[db] = (f32x16)0.f; dv[db] = (f32x16)0.f; }
+    Unit unit{LEAST_UNIT};
+    LaneReads<DP> at;
+    at.start(lane);
+
     // the next tile to load: tokens ft .. of head fh; the last tiles of tokens end at t.hi, the first may begin before t.lo
     Src src;
     src.start(nullptr, a.q.row, nullptr, a.dout.row, a.dim, wave, lane);
@@ -283,28 +297,6 @@ template <class T, int DP> __global__ __launch_bounds__(DP == 128 ? 512 : 256, 2
             ft -= RT;
         }
     };
-    const int t0_first = max(ft, 0), tt_first = ft, th_first = fh;
-    if (begin < end)
-        for (int x = 0; x < AHEAD; ++x) fetch(x);      // on their way before k and v are read
-
-    s16x8 k[KS], v[V_LDS ? 1 : KS];
-    f32x16 dk[DB], dv[DB];
-#pragma unroll
-    for (int ks = 0; ks < KS; ++ks) {
-        k[ks] = __builtin_bit_cast(s16x8, load_piece<DP>(a.k.p, (int64_t)(s.k0 + kept) * a.k.row + (int64_t)hk * a.k.head, 2 * ks + (lane >> 5), a.dim));
-        if (!V_LDS) v[V_LDS ? 0 : ks] = __builtin_bit_cast(s16x8, load_piece<DP>(a.v.p, (int64_t)(s.k0 + kept) * a.v.row + (int64_t)hk * a.v.head, 2 * ks + (lane >> 5), a.dim));
-    }
-    if (V_LDS)
-        for (int at = tid; at < 128 * (DP / 8); at += THREADS) {
-            const int r = at / (DP / 8), piece = at % (DP / 8);
-            *(u32x4 *)(vt + tile_at<DP>(r, piece)) = load_piece<DP>(a.v.p, (int64_t)(s.k0 + min(k0 + r, s.nk - 1)) * a.v.row + (int64_t)hk * a.v.head, piece, a.dim);
-        }
-#pragma unroll
-    for (int db = 0; db < DB; ++db) { dk[db] = (f32x16)0.f; dv[db] = (f32x16)0.f; }
-    Unit unit{LEAST_UNIT};
-    LaneReads<DP> at;
-    at.start(lane);
-
     constexpr int LOADS = 2 * Src::COUNT + 2;    // of a wave to a tile
     static_assert(Src::STEP <= RT, "every wave has rows of a tile to load");
     // waits for the loads of a tile, the AHEAD - 1 tiles after it stay under way; where the mask cuts it for the block, q and dO are cleaned
@@ -321,7 +313,8 @@ template <class T, int DP> __global__ __launch_bounds__(DP == 128 ? 512 : 256, 2
     };
 
     if (begin < end) {
-        int t0 = t0_first, tt = tt_first, th = th_first, slot = 0;
+        int t0 = max(ft, 0), tt = ft, th = fh, slot = 0;
+        for (int x = 0; x < AHEAD; ++x) fetch(x);
         registers_loaded();
         take(t0, 0);
         for (int n = begin; n < end; ++n) {
