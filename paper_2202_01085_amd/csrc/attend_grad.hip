@@ -467,7 +467,8 @@ template <class T> __global__ __launch_bounds__(NT) void join_keys(AttendArgs a)
 
 // How grad_keys is cut.  A block has a CU to itself at head sizes above 64, half of one below: 256 or 512 run at a time.  Key tiles are
 // cut into parts where there are too few of them to fill and even out the rounds: the number of parts that makes the shortest time
-// by counting row tiles, and `ends` of them for a block's beginning and end.  With a window all key tiles have about the same rows
+// by counting row tiles (0.5 to 0.8 us each), `ends` of them for a block's beginning and end, and the sum of the parts after it
+// (4 us for a few, 9 for 1024: a call of 10 tokens is not cut, four sequences of 2048 take 296 us whole and 297 cut).  With a window all key tiles have about the same rows
 // (`usual`) but those of the sinks, which all later tokens see and which are always cut to the others' size.
 void cut_keys(AttendArgs &a, int64_t max_k) {
     const int64_t tiles = cdiv(max_k, 128), all = tiles * a.groups, slots = a.dim > 64 ? 256 : 512, ends = a.dim > 64 ? 12 : 4;
@@ -480,8 +481,9 @@ void cut_keys(AttendArgs &a, int64_t max_k) {
     for (int64_t p = 1; p <= 64 && (p == 1 || all * p <= 4 * slots); ++p) {
         const int64_t chunk = cdiv(usual, p), more = sinks * a.groups * std::max<int64_t>(0, cdiv(longest, chunk) - p);
         const int64_t rounds = cdiv(all * p + more, slots);
-        const double cost = even ? (double)(rounds * (chunk + ends))
+        double cost = even ? (double)(rounds * (chunk + ends))
                                  : std::max((double)chunk, (double)(all * usual) / (2.0 * (double)slots) + 0.5 * (double)chunk) + (double)(ends * rounds);
+        if (p > 1 && !sinks) cost += 6.0 + (double)(all * p) / 128.0;
         if (cost < least) {
             least = cost;
             parts = p;
