@@ -366,7 +366,7 @@ template <class T, int DP, bool E8> __global__ __launch_bounds__(NT, E8 ? 2 : 1)
     const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6);
     const Limits first = limits_of(a, s, r0 / a.group), last = limits_of(a, s, min(r0 + 31, rows - 1) / a.group);
     const Tiles tiles = tiles_of<N>(first, last, a.sinks);
-    const int begin = it.part * a.chunk, end = a.parts > 1 ? min(tiles.count, begin + a.chunk) : tiles.count;
+    const int begin = it.part * a.chunk, end = min(tiles.count, begin + a.chunk);   // also of one part: pages[] holds no more
     const int row = min(r0 + (lane & 31), rows - 1), token = row / a.group, head = hk * a.group + row % a.group;
     const bool valid = r0 + (lane & 31) < rows;
     const int64_t at_row = (int64_t)(s.q0 + token) * a.heads + head;

@@ -138,6 +138,25 @@ def test_long_texts(news, lengths, Hq, Hk):
     check(BF, BF, news, lengths, Hq, Hk, 64, 32, window=5000, sinks=2, seed=4)
 
 
+def test_a_max_k_that_is_too_small():
+    """lengths past max_k: that sequence's results are not defined, but nothing else is touched, and other sequences are right"""
+    D, page, lengths = 64, 8, [30000, 100]
+    c, table, k, v = filled(BF, E8, lengths, 1, D, page, 21)
+    q = normal((2, 2, D), 3, BF)
+    before = c.k.view(torch.uint8).clone()
+    out, lse = c.attention(q.to(DEV), table, torch.tensor(lengths, dtype=torch.int32, device=DEV), max_k=128)
+    want = au.batch(q[1:], k[30000:], v[30000:], [0, 1], [0, 100], 0.125)
+    au.close(out[1:], want, "out")
+    au.close(lse[1:], want, "lse")
+    assert torch.equal(before, c.k.view(torch.uint8))
+
+
+def test_more_than_256_parts():
+    """one head over a very long text: the parts' weights are read in several rounds"""
+    check(BF, E8, [1], [140001], 1, 1, 32, 64, seed=8, max_k=140001)
+    check(HF, HF, [1], [300000], 1, 1, 32, 128, seed=9, max_k=300000)
+
+
 def test_empty_sequences_and_more_tokens_than_keys():
     check(BF, E8, [3, 1, 5], [0, 1, 2], 4, 2, 64, 16)
 
