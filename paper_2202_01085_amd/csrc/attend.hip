@@ -700,6 +700,7 @@ void run_attend(AttendArgs a, int64_t max_k, bool f16, bool e8, void *workspace,
     a.part_out = (float *)workspace;
     a.part_lse = a.part_out ? a.part_out + (int64_t)a.parts * a.total_q * a.heads * a.dim : nullptr;
     const int64_t blocks = attend_blocks(a, (int64_t)a.tiles * a.parts);
+    if (a.parts > 1 && cdiv(a.total_q * a.heads, 8) >= 1 << 24) fail(F3M_ERR_UNSUPPORTED, "attention: too many rows to join parts of in one call (2^27)");
     f16 ? launch_dim<F16>(a, e8, few, blocks, st) : launch_dim<Bf16>(a, e8, few, blocks, st);
 }
 

@@ -507,19 +507,24 @@ int64_t key_items(const AttendArgs &a) {
 int64_t stat_floats(const AttendArgs &a) { return cdiv(2 * a.total_q * a.heads, 64) * 64; }
 
 template <class T, int DP> void launch(AttendArgs a, int64_t max_k, hipStream_t st) {
+    AttendArgs keys = a;                       // what cannot be launched is refused before anything is
+    int64_t key_blocks = 0;
+    if (max_k && a.total_k) {
+        cut_keys(keys, max_k);
+        key_blocks = attend_blocks(keys, key_items(keys));
+        if ((int64_t)keys.groups * keys.split * 16 >= 1 << 24) fail(F3M_ERR_UNSUPPORTED, "attention: too many sequences for one call's gradients");
+    }
     if (a.max_q && a.total_q) {
         a.tiles = (int)cdiv((int64_t)a.max_q * a.group, 128);
         const int64_t blocks = attend_blocks(a, a.tiles);
         grad_rows<T, DP><<<dim3((uint32_t)blocks), NT, 0, st>>>(a);
         F3M_HIP(hipGetLastError());
     }
-    if (max_k && a.total_k) {
-        cut_keys(a, max_k);
-        const int64_t blocks = attend_blocks(a, key_items(a));
-        grad_keys<T, DP><<<dim3((uint32_t)blocks), DP == 128 ? 512 : 256, 0, st>>>(a);
+    if (key_blocks) {
+        grad_keys<T, DP><<<dim3((uint32_t)key_blocks), DP == 128 ? 512 : 256, 0, st>>>(keys);
         F3M_HIP(hipGetLastError());
-        if (a.split) {
-            join_keys<T><<<dim3((uint32_t)((int64_t)a.groups * a.split * 16)), NT, 0, st>>>(a);
+        if (keys.split) {
+            join_keys<T><<<dim3((uint32_t)((int64_t)keys.groups * keys.split * 16)), NT, 0, st>>>(keys);
             F3M_HIP(hipGetLastError());
         }
     }

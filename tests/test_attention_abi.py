@@ -131,6 +131,15 @@ def test_cache_calls_that_are_refused(lib):
     assert lib.f3m_cache_attention(c, ctypes.byref(args(total_q=0)), FAKE, 4, 4, FAKE, None, None, None, 0, None) == 0
 
 
+def test_joins_of_more_blocks_than_a_grid_has_are_refused(lib):
+    one = dict(heads=1, kv_heads=1)
+    a = ctypes.byref(args(max_q=1, max_k=100000, total_q=2 ** 27, total_k=100000, **one))
+    assert lib.f3m_attention(a, ctypes.byref(OUT), FAKE, FAKE, 1 << 60, None) == UNSUPPORTED
+    a = ctypes.byref(args(batch=2 ** 20, q_offsets=FAKE, k_offsets=FAKE, window=1, sinks=1, max_q=512, max_k=128, total_q=2 ** 20, total_k=2 ** 20, **one))
+    r = [ctypes.byref(x) for x in (OUT, OUT, OUT, KV, KV)]
+    assert lib.f3m_attention_grad(a, r[0], r[1], FAKE, r[2], r[3], r[4], FAKE, 1 << 60, None) == UNSUPPORTED
+
+
 def test_host_tensors_are_refused():
     x = torch.zeros((4, 2, 64), dtype=torch.bfloat16)
     with pytest.raises(TypeError):
