@@ -297,8 +297,9 @@ f3m_status f3m_cg_solve(f3m_plan_t *plan, float lambda, const float *b, float *x
  * (p < 0) gets o = 0 and lse = -inf, and adds nothing to the gradients.  What hidden keys hold (NaN, infinities)
  * reaches no token, nor do hidden tokens' values reach a key's gradients.  A NaN or infinity in a visible row of v makes at
  * least the same elements of o NaN or infinite, one in k, q or dout all that depends on the pair.
- * Offsets and lengths are read on the device and not checked by the host: such as lie outside the tensors or fall are
- * cut to what exists, no access leaves the tensors.
+ * Offsets and lengths are read on the device and not checked by the host: such as lie outside the tensors are cut to
+ * what exists, and no access leaves the tensors.  Offsets do not fall; if they do, results are not defined.
+ * A row whose visible scores are all -inf counts as one that sees no key.
  * Limits: head_dim a multiple of 8 up to 128; data 16-byte aligned, strides multiples of 8 values, those between rows
  * below 2^22; fewer than 2^31 - 65536 rows.
  * Every call is asynchronous on `stream` and allocates nothing; the caller brings the workspace (the *_workspace calls
@@ -350,7 +351,8 @@ f3m_status f3m_attention_grad(const f3m_attention_args *args, const f3m_rows *do
                               int64_t workspace_bytes, void *stream);
 
 /*
- * A cache of k and v in pages, for sequences that grow.  Device memory of the caller, contiguous:
+ * A cache of k and v in pages, for sequences that grow.  Device memory of the caller, contiguous,
+ * k and v 16-byte, exponents 4-byte aligned:
  *   k, v          pages x kv_heads x page_size x head_dim values of type `held`
  *   k_exp, v_exp  pages x kv_heads x page_size bytes, with F3M_E4M3 only (else NULL)
  * Slot s is row s % page_size of page s / page_size.  held = F3M_E4M3: a row's values are code * 2^(byte - 127); the byte is the
@@ -371,6 +373,7 @@ typedef struct {
  * type) to slots[tokens] (device).  A slot below 0 or past the last page is skipped.  Slots of one call differ: of a slot given twice
  * the contents are not defined.
  * f3m_cache_read - the reverse, with zeros for such slots.
+ * Below 2^27 - 8 rows (tokens * kv_heads) to a call.
  */
 f3m_status f3m_cache_write(const f3m_cache *cache, int dtype, const f3m_rows *k, const f3m_rows *v, const int64_t *slots,
                            int64_t tokens, void *stream);

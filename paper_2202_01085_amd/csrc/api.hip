@@ -123,6 +123,8 @@ f3m_status check_cache(const f3m_cache *c) {
         if (!c->k || !c->v) return set_error(F3M_ERR_INVALID_ARG, "k or v of the cache is null");
         if ((uintptr_t)c->k % 16 || (uintptr_t)c->v % 16) return set_error(F3M_ERR_INVALID_ARG, "the cache's data must be 16-byte aligned");
         if (c->held == F3M_E4M3 && (!c->k_exp || !c->v_exp)) return set_error(F3M_ERR_INVALID_ARG, "an 8-bit cache needs k_exp and v_exp");
+        if (c->held == F3M_E4M3 && ((uintptr_t)c->k_exp % 4 || (uintptr_t)c->v_exp % 4))
+            return set_error(F3M_ERR_INVALID_ARG, "k_exp and v_exp must be 4-byte aligned");
     }
     return F3M_OK;
 }

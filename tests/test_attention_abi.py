@@ -105,6 +105,13 @@ def test_caches_that_are_refused(lib, more, status):
     assert lib.f3m_cache_attention(c, ctypes.byref(args()), FAKE, 4, 4, FAKE, ctypes.byref(OUT), FAKE, FAKE, 1 << 40, None) == status
 
 
+@pytest.mark.parametrize("more", [dict(k_exp=FAKE + 2), dict(v_exp=FAKE + 1)])
+def test_exponents_are_read_in_words(lib, more):
+    c, r = ctypes.byref(cache(**more)), ctypes.byref(KV)
+    assert lib.f3m_cache_write(c, 0, r, r, FAKE, 5, None) == INVALID
+    assert lib.f3m_cache_attention(c, ctypes.byref(args()), FAKE, 4, 4, FAKE, ctypes.byref(OUT), FAKE, FAKE, 1 << 40, None) == INVALID
+
+
 def test_cache_calls_that_are_refused(lib):
     c, r, ok, out = ctypes.byref(cache()), ctypes.byref(KV), ctypes.byref(args()), ctypes.byref(OUT)
     for call in (lib.f3m_cache_write, lib.f3m_cache_read):
