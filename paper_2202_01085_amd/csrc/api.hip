@@ -150,7 +150,7 @@ f3m::AttendArgs attend_args(const f3m_attention_args &p) {
     a.dim = p.head_dim;
     a.causal = p.causal != 0;
     a.window = p.window;
-    a.sinks = p.window ? p.sinks : 0;
+    a.sinks = p.window ? std::min(p.sinks, INT32_MAX - 65536) : 0;   // more keys than a sequence has; rounded up to tiles it stays an int
     a.scale = p.scale;
     a.total_q = p.total_q;
     a.total_k = p.total_k;

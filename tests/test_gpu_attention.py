@@ -338,3 +338,9 @@ def test_binding_refuses():
     with pytest.raises(f3m.F3MError) as e:
         f3m.attention(torch.zeros((4, 2, 136), dtype=BF, device=DEV), *[torch.zeros((4, 2, 136), dtype=BF, device=DEV)] * 2)
     assert e.value.status == 3
+
+
+@pytest.mark.parametrize("sinks", [300, 2 ** 31 - 64, 2 ** 31 - 1])
+def test_sinks_past_the_sequence(sinks):
+    run(BF, 32, 2, 2, [300, 3], window=7, sinks=sinks)
+    run(BF, 32, 2, 1, [3], [300], window=7, sinks=sinks)
