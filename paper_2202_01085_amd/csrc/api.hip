@@ -93,12 +93,12 @@ f3m_status check_rows(const f3m_rows &r, int64_t rows, const char *name) {
 }
 
 // results do not overlap themselves: one stride steps over all that the other spans
-f3m_status check_result(const f3m_rows *r, const f3m_attention_args &p, int64_t rows, int heads, const char *name) {
+f3m_status check_result(const f3m_rows *r, int dim, int64_t rows, int heads, const char *name) {
     if (!r) return set_error(F3M_ERR_INVALID_ARG, std::string(name) + " is null");
     f3m_status st = check_rows(*r, rows, name);
     if (st != F3M_OK) return st;
-    const bool by_row = (heads == 1 || r->head >= p.head_dim) && (rows == 1 || r->row >= (heads - 1) * (heads == 1 ? 0 : r->head) + p.head_dim);
-    const bool by_head = (rows == 1 || r->row >= p.head_dim) && (heads == 1 || r->head >= (rows - 1) * (rows == 1 ? 0 : r->row) + p.head_dim);
+    const bool by_row = (heads == 1 || r->head >= dim) && (rows == 1 || r->row >= (heads - 1) * (heads == 1 ? 0 : r->head) + dim);
+    const bool by_head = (rows == 1 || r->row >= dim) && (heads == 1 || r->head >= (rows - 1) * (rows == 1 ? 0 : r->row) + dim);
     if (!by_row && !by_head) return set_error(F3M_ERR_INVALID_ARG, std::string(name) + ": rows that are written must not overlap");
     return F3M_OK;
 }
@@ -366,7 +366,7 @@ f3m_status f3m_attention(const f3m_attention_args *args, const f3m_rows *out, fl
         st = check_rows(args->q, args->total_q, "q");
         if (st == F3M_OK && args->total_k > 0) st = check_rows(args->k, args->total_k, "k");
         if (st == F3M_OK && args->total_k > 0) st = check_rows(args->v, args->total_k, "v");
-        if (st == F3M_OK) st = check_result(out, *args, args->total_q, args->heads, "out");
+        if (st == F3M_OK) st = check_result(out, args->head_dim, args->total_q, args->heads, "out");
         if (st == F3M_OK && !lse) st = set_error(F3M_ERR_INVALID_ARG, "lse is null");
     }
     if (st != F3M_OK || args->total_q == 0 || args->batch == 0) return st;
@@ -388,13 +388,13 @@ f3m_status f3m_attention_grad(const f3m_attention_args *args, const f3m_rows *do
         st = check_rows(args->q, args->total_q, "q");
         if (st == F3M_OK) st = check_rows(*dout, args->total_q, "dout");
         if (st == F3M_OK) st = check_rows(*out, args->total_q, "out");
-        if (st == F3M_OK) st = check_result(dq, *args, args->total_q, args->heads, "dq");
+        if (st == F3M_OK) st = check_result(dq, args->head_dim, args->total_q, args->heads, "dq");
     }
     if (st == F3M_OK && args->total_k > 0) {
         st = check_rows(args->k, args->total_k, "k");
         if (st == F3M_OK) st = check_rows(args->v, args->total_k, "v");
-        if (st == F3M_OK) st = check_result(dk, *args, args->total_k, args->kv_heads, "dk");
-        if (st == F3M_OK) st = check_result(dv, *args, args->total_k, args->kv_heads, "dv");
+        if (st == F3M_OK) st = check_result(dk, args->head_dim, args->total_k, args->kv_heads, "dk");
+        if (st == F3M_OK) st = check_result(dv, args->head_dim, args->total_k, args->kv_heads, "dv");
     }
     if (st != F3M_OK) return st;
     f3m::AttendArgs a = attend_args(*args);
@@ -424,8 +424,9 @@ f3m_status f3m_cache_read(const f3m_cache *cache, int dtype, const f3m_rows *k, 
                           void *stream) {
     f3m_status st = check_cache_rows(cache, dtype, k, v, slots, tokens);
     if (st != F3M_OK || tokens == 0) return st;
-    if (k->head < cache->head_dim || k->row < cache->head_dim || v->head < cache->head_dim || v->row < cache->head_dim)
-        return set_error(F3M_ERR_INVALID_ARG, "rows that are written must not overlap");
+    st = check_result(k, cache->head_dim, tokens, cache->kv_heads, "k");
+    if (st == F3M_OK) st = check_result(v, cache->head_dim, tokens, cache->kv_heads, "v");
+    if (st != F3M_OK) return st;
     return guarded([&] { f3m::run_cache_rows(*cache, dtype == F3M_F16, slots, tokens, *k, *v, false, (hipStream_t)stream); });
 }
 
@@ -445,7 +446,7 @@ f3m_status f3m_cache_attention(const f3m_cache *cache, const f3m_attention_args 
     if (args->total_q == 0 || args->batch == 0) return F3M_OK;
     if (!lengths || (table_cols > 0 && !table)) return set_error(F3M_ERR_INVALID_ARG, "table or lengths is null");
     st = check_rows(args->q, args->total_q, "q");
-    if (st == F3M_OK) st = check_result(out, *args, args->total_q, args->heads, "out");
+    if (st == F3M_OK) st = check_result(out, args->head_dim, args->total_q, args->heads, "out");
     if (st != F3M_OK) return st;
     if (!lse) return set_error(F3M_ERR_INVALID_ARG, "lse is null");
     f3m::AttendArgs a = attend_args(*args);

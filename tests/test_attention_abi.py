@@ -138,6 +138,13 @@ def test_cache_calls_that_are_refused(lib):
     assert lib.f3m_cache_attention(c, ctypes.byref(args(total_q=0)), FAKE, 4, 4, FAKE, None, None, None, 0, None) == 0
 
 
+def test_rows_read_from_a_cache_do_not_overlap(lib):
+    c, ok = ctypes.byref(cache()), ctypes.byref(KV)
+    for rows in (f3m.Rows(FAKE, 64, 64), f3m.Rows(FAKE, 64, 128), f3m.Rows(FAKE, 128, 120)):      # 5 rows of 2 heads of 64
+        assert lib.f3m_cache_read(c, 0, ctypes.byref(rows), ok, FAKE, 5, None) == INVALID
+        assert lib.f3m_cache_read(c, 0, ok, ctypes.byref(rows), FAKE, 5, None) == INVALID
+
+
 def test_joins_of_more_blocks_than_a_grid_has_are_refused(lib):
     one = dict(heads=1, kv_heads=1)
     a = ctypes.byref(args(max_q=1, max_k=100000, total_q=2 ** 27, total_k=100000, **one))
