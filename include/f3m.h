@@ -304,7 +304,7 @@ f3m_status f3m_cg_solve(f3m_plan_t *plan, float lambda, const float *b, float *x
  * below 2^22; fewer than 2^31 - 65536 rows.
  * Every call is asynchronous on `stream` and allocates nothing; the caller brings the workspace (the *_workspace calls
  * say how many bytes) and gives each call that may run at the same time its own.  Any call may be captured into a HIP
- * graph.  Sums are made in a fixed order: results repeat bit for bit.
+ * graph.  Sums are made in a fixed order: results repeat bit for bit.  What a call writes overlaps neither what it reads nor itself.
  */
 typedef enum { F3M_BF16 = 0, F3M_F16 = 1, F3M_E4M3 = 2 } f3m_dtype;
 
@@ -363,7 +363,7 @@ f3m_status f3m_attention_grad(const f3m_attention_args *args, const f3m_rows *do
 typedef struct {
     int32_t held;              /* F3M_BF16, F3M_F16 or F3M_E4M3 */
     int32_t kv_heads, head_dim, page_size;
-    int64_t pages;             /* pages * page_size below 2^40 */
+    int64_t pages;             /* pages * page_size below 2^40, kv_heads * page_size below 2^31 */
     void *k, *v;
     uint8_t *k_exp, *v_exp;
 } f3m_cache;

@@ -118,6 +118,7 @@ f3m_status check_cache(const f3m_cache *c) {
     if (c->head_dim > 128) return set_error(F3M_ERR_UNSUPPORTED, "head_dim above 128 is not supported");
     if (c->page_size < 8 || c->page_size > 1024 || (c->page_size & (c->page_size - 1)))
         return set_error(F3M_ERR_INVALID_ARG, "page_size must be a power of two from 8 to 1024");
+    if ((int64_t)c->kv_heads * c->page_size >= (int64_t)1 << 31) return set_error(F3M_ERR_UNSUPPORTED, "kv_heads * page_size must be below 2^31");
     if (c->pages < 0 || c->pages >= ((int64_t)1 << 40) / c->page_size) return set_error(F3M_ERR_INVALID_ARG, "pages * page_size must be in [0, 2^40)");
     if (c->pages > 0) {
         if (!c->k || !c->v) return set_error(F3M_ERR_INVALID_ARG, "k or v of the cache is null");

@@ -145,6 +145,11 @@ def test_rows_read_from_a_cache_do_not_overlap(lib):
         assert lib.f3m_cache_read(c, 0, ok, ctypes.byref(rows), FAKE, 5, None) == INVALID
 
 
+def test_pages_past_32_bits_are_refused(lib):
+    c, r = ctypes.byref(cache(kv_heads=2 ** 21, page_size=1024)), ctypes.byref(KV)
+    assert lib.f3m_cache_write(c, 0, r, r, FAKE, 5, None) == UNSUPPORTED
+
+
 def test_joins_of_more_blocks_than_a_grid_has_are_refused(lib):
     one = dict(heads=1, kv_heads=1)
     a = ctypes.byref(args(max_q=1, max_k=100000, total_q=2 ** 27, total_k=100000, **one))
