@@ -45,7 +45,11 @@ struct Unit {
 };
 constexpr float LEAST_UNIT = 0x1p-100f;
 
-// dQ: 128 rows of one group to a block, 32 to a wave, tiles of 64 keys through LDS, as the forward kernel.  It also leaves each row's
+// Parts of a tile of `count` steps: `chunk` each, the last one what is left
+__device__ __forceinline__ int parts_of(int count, int chunk, int most) { return min(max(count - 1, 0) / chunk + 1, most); }
+
+// dQ: 128 rows of one group to a block, 32 to a wave, tiles of 64 keys through LDS, as the forward kernel.  Few row tiles are cut into parts
+// along the keys (cut_rows), whose fp32 sums join_rows adds up.  It also leaves each row's
 // stat for grad_keys: -log2 of its sum (+ LIFT), or -inf for an empty row, so that its weights are 0, and -dO.O.
 template <class T, int DP> __global__ __launch_bounds__(NT, 2) void grad_rows(AttendArgs a) {
     constexpr int KS = DP / 16, DB = DP / 32, KT = 64;
@@ -59,6 +63,9 @@ template <class T, int DP> __global__ __launch_bounds__(NT, 2) void grad_rows(At
     const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6);
     const Limits first = limits_of(a, s, r0 / a.group), last = limits_of(a, s, min(r0 + 127, rows - 1) / a.group);
     const Tiles tiles = tiles_of<KT>(first, last, a.sinks);
+    const int parts = parts_of(tiles.count, a.chunk, a.parts);
+    if (it.part >= parts) return;
+    const int begin = it.part * a.chunk, end = it.part + 1 < parts ? begin + a.chunk : tiles.count;
 
     const int w0 = r0 + 32 * wave, row = min(w0 + (lane & 31), rows - 1), token = row / a.group, head = hk * a.group + row % a.group;
     const bool valid = w0 + (lane & 31) < rows, idle = w0 >= rows;
@@ -125,7 +132,7 @@ template <class T, int DP> __global__ __launch_bounds__(NT, 2) void grad_rows(At
         delta = -both_halves_sum(sum);
         __syncthreads();
     }
-    if (valid && lane < 32) {
+    if (it.part == 0 && valid && lane < 32) {
         const int64_t x = (int64_t)head * a.total_q + s.q0 + token;
         a.stat[x] = less + LIFT<T>;
         a.stat[x + (int64_t)a.heads * a.total_q] = delta;
@@ -152,7 +159,7 @@ template <class T, int DP> __global__ __launch_bounds__(NT, 2) void grad_rows(At
 #pragma unroll
         for (int db = 0; db < DB; ++db) acc[db] = (f32x16)0.f;
         unit.u = LEAST_UNIT;
-        if (tiles.count == 0) return;
+        if (begin >= end) return;
         // waits for the loads of tile t
         auto take = [&](int t, int buf) {
             arrived();
@@ -162,19 +169,19 @@ template <class T, int DP> __global__ __launch_bounds__(NT, 2) void grad_rows(At
             clean_tile<T, DP, KT>(tile[buf][0], tid);
             __syncthreads();
         };
-        fetch(0, 0);
+        fetch(begin, begin & 1);
         registers_loaded();
-        take(0, 0);
-        for (int n = 0; n < tiles.count; ++n) {
+        take(begin, begin & 1);
+        for (int n = begin; n < end; ++n) {
             const int buf = n & 1, key0 = tiles[n] * KT;
-            if (n + 1 < tiles.count) fetch(n + 1, buf ^ 1);
+            if (n + 1 < end) fetch(n + 1, buf ^ 1);
             const bool none = idle || key0 >= wlast.hi || (key0 + KT <= wfirst.lo && key0 >= a.sinks);
             const bool full = key0 + KT <= wfirst.hi && (key0 >= wlast.lo || key0 + KT <= a.sinks);
             if (!none) {
                 block(lds_address(tile[buf][0]), lds_address(tile[buf][1]), 0, key0, !full);
                 block(lds_address(tile[buf][0]), lds_address(tile[buf][1]), 1, key0, !full);
             }
-            if (n + 1 < tiles.count) take(n + 1, buf ^ 1);
+            if (n + 1 < end) take(n + 1, buf ^ 1);
         }
     };
     pass(false);
@@ -185,7 +192,38 @@ template <class T, int DP> __global__ __launch_bounds__(NT, 2) void grad_rows(At
         for (int i = 0; i < 16; ++i) finite &= fabsf(acc[db][i]) < __builtin_inff();
     if (__syncthreads_or(!finite)) pass(true);
     const float by = T::narrow ? a.scale * unit.u : a.scale;
+    if (parts > 1) {     // fp32 sums of this part, for join_rows
+        if (!valid) return;
+        float *to_part = a.part_out + ((((int64_t)it.group * a.tiles + it.tile) * a.parts + it.part) * 128 + 32 * wave + (lane & 31)) * a.dim;
+#pragma unroll
+        for (int db = 0; db < DB; ++db)
+#pragma unroll
+            for (int i = 0; i < 16; i += 4) {
+                const int x = 32 * db + c_row(i, lane);
+                if (x < a.dim) *(float4 *)(to_part + x) = make_float4(acc[db][i] * by, acc[db][i + 1] * by, acc[db][i + 2] * by, acc[db][i + 3] * by);
+            }
+        return;
+    }
     store_rows<T, DB>(acc, by, a.dq.p, (int64_t)(s.q0 + token) * a.dq.row + (int64_t)head * a.dq.head, a.dim, valid, lane);
+}
+
+// the parts of the row tiles that were cut, summed in their order: a block to 8 rows of a tile, 32 lanes to a row, 4 values each
+template <class T> __global__ __launch_bounds__(NT) void join_rows(AttendArgs a) {
+    const int group = blockIdx.x / (16 * a.tiles), at_tile = blockIdx.x / 16 % a.tiles, in = blockIdx.x % 16 * 8 + threadIdx.x / 32, x = threadIdx.x % 32 * 4;
+    const int b = group / a.kv_heads, hk = group % a.kv_heads, r0 = at_tile * 128;
+    const Sequence s = sequence_of(a, b);
+    const int rows = min(s.nq, a.max_q) * a.group;
+    if (r0 + in >= rows || x >= a.dim) return;
+    const int parts = parts_of(tiles_of<64>(limits_of(a, s, r0 / a.group), limits_of(a, s, min(r0 + 127, rows - 1) / a.group), a.sinks).count, a.chunk, a.parts);
+    if (parts == 1) return;
+    const float *from = a.part_out + ((((int64_t)group * a.tiles + at_tile) * a.parts) * 128 + in) * a.dim + x;
+    float4 q = make_float4(0.f, 0.f, 0.f, 0.f);
+    for (int p = 0; p < parts; ++p, from += (int64_t)128 * a.dim) {
+        const float4 y = *(const float4 *)from;
+        q.x += y.x; q.y += y.y; q.z += y.z; q.w += y.w;
+    }
+    const int token = (r0 + in) / a.group, head = hk * a.group + (r0 + in) % a.group;
+    *(u32x2 *)(a.dq.p + 2 * ((int64_t)(s.q0 + token) * a.dq.row + (int64_t)head * a.dq.head + x)) = (u32x2){T::pack(q.x, q.y), T::pack(q.z, q.w)};
 }
 
 // A block of grad_keys: 128 keys of a group and the row tiles that see them, RT tokens of one head each: the heads of the group for the
@@ -207,6 +245,11 @@ __device__ __forceinline__ KeyTile key_tile(const AttendArgs &a, const Sequence 
     }
     t.count = (t.hi - t.lo + RT - 1) / RT * a.group;
     return t;
+}
+
+// parts of a key tile
+__device__ __forceinline__ int key_parts(const AttendArgs &a, int at_tile, int count) {
+    return at_tile < a.split ? parts_of(count, a.chunk, at_tile < (a.sinks + 127) / 128 ? a.parts : a.usual) : 1;
 }
 
 // dK, dV: 32 keys to a wave, whose sums stay in registers; tiles of q and dO come through a ring in LDS, two or more under way while one
@@ -238,10 +281,9 @@ template <class T, int DP> __global__ __launch_bounds__(DP == 128 ? 512 : 256, 2
     const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6), kw = wave & 3, half = wave >> 2;
     const int off = s.nk - s.nq;                                     // position of token 0
     const KeyTile t = key_tile(a, s, k0, min(k0 + 128, s.nk));
-    const bool cut = at_tile < a.split && t.count > a.chunk;
-    if (!cut && it.part > 0) return;
-    const int begin = cut ? it.part * a.chunk : 0, end = cut ? min(t.count, begin + a.chunk) : t.count;
-    if (cut && begin >= end) return;
+    const int parts = key_parts(a, at_tile, t.count);
+    if (it.part >= parts) return;
+    const int begin = it.part * a.chunk, end = it.part + 1 < parts ? begin + a.chunk : t.count;
 
     const int w0 = k0 + 32 * kw, key = w0 + (lane & 31), kept = min(key, s.nk - 1);
     const bool valid = key < s.nk, idle = w0 >= s.nk;
@@ -427,7 +469,7 @@ template <class T, int DP> __global__ __launch_bounds__(DP == 128 ? 512 : 256, 2
         if (half == 1) return;
     }
     const int64_t row = s.k0 + kept;
-    if (cut) {     // fp32 sums of this part, for join_keys
+    if (parts > 1) {     // fp32 sums of this part, for join_keys
         float *to_part = a.part_out + ((((int64_t)it.group * a.split + at_tile) * a.parts + it.part) * 256 + 32 * kw + (lane & 31)) * a.dim;
 #pragma unroll
         for (int db = 0; db < DB; ++db)
@@ -451,8 +493,8 @@ template <class T> __global__ __launch_bounds__(NT) void join_keys(AttendArgs a)
     const Sequence s = sequence_of(a, b);
     if (k0 + in >= s.nk || x >= a.dim) return;
     const KeyTile t = key_tile(a, s, k0, min(k0 + 128, s.nk));
-    if (t.count <= a.chunk) return;
-    const int parts = (t.count + a.chunk - 1) / a.chunk;
+    const int parts = key_parts(a, at_tile, t.count);
+    if (parts == 1) return;
     const float *from = a.part_out + ((((int64_t)group * a.split + at_tile) * a.parts) * 256 + in) * a.dim + x;
     float4 k = make_float4(0.f, 0.f, 0.f, 0.f), v = k;
     for (int p = 0; p < parts; ++p, from += (int64_t)256 * a.dim) {
@@ -465,37 +507,62 @@ template <class T> __global__ __launch_bounds__(NT) void join_keys(AttendArgs a)
     *(u32x2 *)(a.dv.p + 2 * (row * a.dv.row + (int64_t)hk * a.dv.head + x)) = (u32x2){T::pack(v.x, v.y), T::pack(v.z, v.w)};
 }
 
-// How grad_keys is cut.  A block has a CU to itself at head sizes above 64, half of one below: 256 or 512 run at a time.  Key tiles are
-// cut into parts where there are too few of them to fill and even out the rounds: the number of parts that makes the shortest time
-// by counting row tiles (0.5 to 0.8 us each), `ends` of them for a block's beginning and end, and the sum of the parts after it
-// (4 us for a few, 9 for 1024: a call of 10 tokens is not cut, four sequences of 2048 take 296 us whole and 297 cut).  With a window all key tiles have about the same rows
-// (`usual`) but those of the sinks, which all later tokens see and which are always cut to the others' size.
+// tiles of 128 rows of all groups: `tiles` in the longest sequence, at most as many as all rows make
+int64_t all_tiles(const AttendArgs &a, int64_t tiles, int64_t rows) {
+    return std::max<int64_t>(1, std::min(tiles * a.groups, (rows / 128 + a.batch) * a.kv_heads));
+}
+
+// How grad_keys is cut.  A block has a CU to itself at head sizes above 64, half of one below: 256 or 512 places.  Blocks go to the XCDs in
+// turn, whatever their length, so that a little more than one round of them takes as long as two.
+// With a window, without order or with few tokens after many keys, tiles are about equally long (`usual`) but those of the sinks, which
+// all later tokens see and which are always cut to the others' size.  There the parts are those of the shortest time by counting rounds
+// and steps, `ends` of them for a block's beginning and end and what the sum of the parts takes; a step is 2 us, 1 us up to 64.
+// Else lengths fall to nothing along the keys, and p parts of the longest tile make (p + 1) / 2 to a tile: as many as fill 88 % of one
+// round or, if that is fewer than three, two, whose second ones are what others lack.  All gradients of 6709 tokens, 4 heads, one key
+// head: 692 us whole, 397 in 2 parts, 249 in 4, 202 in 6, 232 in 8; of 4 x 2048, 16 heads, 4 key heads: 322, 286 in 2, 296 in 3, 326 in 4.
 void cut_keys(AttendArgs &a, int64_t max_k) {
-    const int64_t tiles = cdiv(max_k, 128), all = tiles * a.groups, slots = a.dim > 64 ? 256 : 512, ends = a.dim > 64 ? 12 : 4;
+    const int64_t tiles = cdiv(max_k, 128), all = all_tiles(a, tiles, a.total_k), places = a.dim > 64 ? 256 : 512, ends = a.dim > 64 ? 12 : 4;
     const int64_t longest = std::max<int64_t>(1, cdiv(a.max_q, RT) * a.group);
     const int64_t usual = a.window ? std::min(longest, (cdiv((int64_t)a.window + 128, RT) + 1) * a.group) : longest;
     const int64_t sinks = usual < longest ? std::min(tiles, cdiv(a.sinks, 128)) : 0;
-    const bool even = usual < longest || !a.causal;      // else lengths fall to nothing along the keys
     int64_t parts = 1;
-    double least = 1e30;
-    for (int64_t p = 1; p <= 64 && (p == 1 || all * p <= 4 * slots); ++p) {
-        const int64_t chunk = cdiv(usual, p), more = sinks * a.groups * std::max<int64_t>(0, cdiv(longest, chunk) - p);
-        const int64_t rounds = cdiv(all * p + more, slots);
-        double cost = even ? (double)(rounds * (chunk + ends))
-                                 : std::max((double)chunk, (double)(all * usual) / (2.0 * (double)slots) + 0.5 * (double)chunk) + (double)(ends * rounds);
-        if (p > 1 && !sinks) cost += 6.0 + (double)(all * p) / 128.0;
-        if (cost < least) {
-            least = cost;
-            parts = p;
+    if (usual < longest || !a.causal || 2 * (int64_t)a.max_q < max_k) {
+        double least = 1e30;
+        for (int64_t p = 1; p <= 64 && (p == 1 || all * p <= 4 * places); ++p) {
+            const int64_t chunk = cdiv(usual, p), more = sinks * a.groups * std::max<int64_t>(0, cdiv(longest, chunk) - p);
+            const double joined = p > 1 && !sinks ? (512.0 + (double)(all * p)) / (a.dim > 64 ? 256.0 : 100.0) : 0.0;
+            const double time = (double)(cdiv(all * p + more, places) * (chunk + ends)) + joined;
+            if (time < least) {
+                least = time;
+                parts = p;
+            }
         }
+    } else {
+        parts = std::min<int64_t>((44 * places / 25 - all) / all, 64);
+        if (parts < 3) parts = all <= places && usual >= 32 ? 2 : 1;
+        parts = std::max<int64_t>(1, std::min(parts, usual / 2));
     }
     const int64_t chunk = cdiv(usual, parts);
     a.tiles = (int)tiles;
     a.chunk = (int)chunk;
-    a.split = (int)(parts > 1 ? tiles : sinks);
     a.usual = (int)cdiv(usual, chunk);
+    a.split = (int)(a.usual > 1 ? tiles : sinks);
     a.parts = (int)std::max<int64_t>(a.usual, a.split ? cdiv(longest, chunk) : 1);
     if (a.parts == 1) a.split = 0;
+}
+
+// How grad_rows is cut, at two blocks to a CU: parts of 10 key tiles or more fill the 512 places, where the row tiles do not; of tiles whose
+// lengths rise along the rows it takes twice as many.  One head over 6709 tokens, 53 row tiles: 150 us whole, 36 + 8 for the sums in
+// 14 parts; four heads, 210: 158 whole, 90 + 9 in 3.  Shorter parts cost as much as they save (4 x 1024 tokens, 16 key tiles, 256 row
+// tiles: all gradients 49 us whole, 61 in two parts).
+void cut_rows(AttendArgs &a, int64_t max_k) {
+    a.tiles = (int)cdiv((int64_t)a.max_q * a.group, 128);
+    const int64_t longest = std::max<int64_t>(1, cdiv(max_k, 64)), items = all_tiles(a, a.tiles, a.total_q * a.group);
+    const int64_t most = a.window ? std::min(longest, cdiv((int64_t)a.window + cdiv(128, a.group), 64) + 1 + cdiv(a.sinks, 64)) : longest;
+    const bool even = most < longest || !a.causal || 2 * (int64_t)a.max_q < max_k;
+    const int64_t parts = std::min({(even ? 511 : 1023) / items, most / 10, (int64_t)64});
+    a.chunk = (int)cdiv(most, std::max<int64_t>(1, parts));
+    a.parts = (int)cdiv(most, a.chunk);
 }
 
 // items of a group: the usual parts of all tiles, the other parts of the sinks' tiles (in rows of `tiles`, as block_of counts)
@@ -509,16 +576,21 @@ int64_t stat_floats(const AttendArgs &a) { return cdiv(2 * a.total_q * a.heads, 
 template <class T, int DP> void launch(AttendArgs a, int64_t max_k, hipStream_t st) {
     AttendArgs keys = a;                       // what cannot be launched is refused before anything is
     int64_t key_blocks = 0;
+    cut_rows(a, max_k);
+    const int64_t row_blocks = attend_blocks(a, (int64_t)a.tiles * a.parts);
+    if (a.parts > 1 && (int64_t)a.groups * a.tiles * 16 >= 1 << 24) fail(F3M_ERR_UNSUPPORTED, "attention: too many sequences for one call's gradients");
     if (max_k && a.total_k) {
         cut_keys(keys, max_k);
         key_blocks = attend_blocks(keys, key_items(keys));
         if ((int64_t)keys.groups * keys.split * 16 >= 1 << 24) fail(F3M_ERR_UNSUPPORTED, "attention: too many sequences for one call's gradients");
     }
     if (a.max_q && a.total_q) {
-        a.tiles = (int)cdiv((int64_t)a.max_q * a.group, 128);
-        const int64_t blocks = attend_blocks(a, a.tiles);
-        grad_rows<T, DP><<<dim3((uint32_t)blocks), NT, 0, st>>>(a);
+        grad_rows<T, DP><<<dim3((uint32_t)row_blocks), NT, 0, st>>>(a);
         F3M_HIP(hipGetLastError());
+        if (a.parts > 1) {
+            join_rows<T><<<dim3((uint32_t)((int64_t)a.groups * a.tiles * 16)), NT, 0, st>>>(a);
+            F3M_HIP(hipGetLastError());
+        }
     }
     if (key_blocks) {
         grad_keys<T, DP><<<dim3((uint32_t)key_blocks), DP == 128 ? 512 : 256, 0, st>>>(keys);
@@ -533,19 +605,22 @@ template <class T, int DP> void launch(AttendArgs a, int64_t max_k, hipStream_t 
 }  // namespace
 
 int64_t attend_grad_workspace(AttendArgs a, int64_t max_k) {
-    int64_t floats = stat_floats(a);
+    int64_t floats = 0;                    // of the parts of either kernel, one after the other
+    if (a.max_q && a.total_q) {
+        cut_rows(a, max_k);
+        if (a.parts > 1) floats = (int64_t)a.groups * a.tiles * a.parts * 128 * a.dim;
+    }
     if (max_k && a.total_k) {
         cut_keys(a, max_k);
-        floats += (int64_t)a.groups * a.split * (a.split ? a.parts : 0) * 256 * a.dim;
+        floats = std::max(floats, (int64_t)a.groups * a.split * (a.split ? a.parts : 0) * 256 * a.dim);
     }
-    return floats * (int64_t)sizeof(float);
+    return (stat_floats(a) + floats) * (int64_t)sizeof(float);
 }
 
 void run_attend_grad(AttendArgs a, int64_t max_k, bool f16, void *workspace, hipStream_t st) {
     if (!a.groups) return;
     a.stat = (float *)workspace;
     a.part_out = a.stat + stat_floats(a);
-    a.parts = 1;
     if (a.dim <= 32) f16 ? launch<F16, 32>(a, max_k, st) : launch<Bf16, 32>(a, max_k, st);
     else if (a.dim <= 64) f16 ? launch<F16, 64>(a, max_k, st) : launch<Bf16, 64>(a, max_k, st);
     else f16 ? launch<F16, 128>(a, max_k, st) : launch<Bf16, 128>(a, max_k, st);

@@ -344,3 +344,34 @@ def test_binding_refuses():
 def test_sinks_past_the_sequence(sinks):
     run(BF, 32, 2, 2, [300, 3], window=7, sinks=sinks)
     run(BF, 32, 2, 1, [3], [300], window=7, sinks=sinks)
+
+
+@pytest.mark.parametrize("type", [BF, HF])
+@pytest.mark.parametrize("D,Hq,Hk,nq,nk,how", [(64, 1, 1, [1900], None, {}), (128, 3, 1, [1400, 1, 650], None, {}), (80, 2, 2, [1300], [1450], {}),
+                                               (40, 2, 1, [1700, 90], None, dict(window=1200, sinks=3)), (128, 1, 1, [1600], None, dict(window=150, sinks=200)),
+                                               (128, 2, 1, [45], [1800], {}), (64, 1, 1, [130, 0], [1500, 70], dict(causal=False))])
+def test_gradients_of_long_sequences_and_few_heads(type, D, Hq, Hk, nq, nk, how):
+    """few tiles of rows and keys: both are cut into parts, whose sums are added up"""
+    run(type, D, Hq, Hk, nq, nk, seed=D + len(nq), **how)
+
+
+def test_gradients_in_parts_past_the_given_maxima():
+    """tokens past max_q and keys past max_k are left out of the gradients, the rest is as without them; again gives the same bits"""
+    n, D = 1500, 64
+    q, k, v, do = (normal((n, 1, D), 60 + i, BF).to(DEV) for i in range(4))
+    off = dev_offsets([0, n])
+    out, lse = f3m.attention(q, k, v)
+    whole = f3m.attention_grad(do, q, k, v, out, lse)
+    grads = [torch.full_like(q, 7.0) for _ in range(3)]
+    for _ in range(2):
+        got = f3m.attention_grad(do, q, k, v, out, lse, q_offsets=off, k_offsets=off, max_q=n, max_k=640, dq=grads[0], dk=grads[1], dv=grads[2])
+        assert all((x[640:] == 7.0).all() for x in got[1:])
+        for x, y in zip(got, whole):      # sums in other parts: in fp32, so no more than a step of bf16 apart, 2^-7 of a value
+            z = torch.where(x == 7.0, y, x).float() - y.float()
+            assert (z.abs() <= 2.0 ** -7 * y.float().abs() + 2.0 ** -12).all()
+    again = f3m.attention_grad(do, q, k, v, out, lse)
+    assert all(torch.equal(x, y) for x, y in zip(again, whole))
+    for x in grads:
+        x.fill_(7.0)
+    f3m.attention_grad(do, q, k, v, out, lse, q_offsets=off, k_offsets=off, max_q=300, max_k=n, dq=grads[0], dk=grads[1], dv=grads[2])
+    assert (grads[0][300:] == 7.0).all() and not (grads[0][:300] == 7.0).all(-1).any()
