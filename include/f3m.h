@@ -335,7 +335,7 @@ int64_t f3m_attention_grad_workspace(const f3m_attention_args *args);
 
 /*
  * f3m_attention - o and lse[row * heads + head] = log sum_j exp(scale q.k_j) (fp32).  The weights are rounded to
- * dtype for the product with v (half a step each, 2^-9 in bf16, 2^-12 in fp16), o once more at the end.
+ * dtype for the product with v (half a step each, 2^-8 in bf16, 2^-11 in fp16), o once more at the end.
  */
 f3m_status f3m_attention(const f3m_attention_args *args, const f3m_rows *out, float *lse, void *workspace,
                          int64_t workspace_bytes, void *stream);
