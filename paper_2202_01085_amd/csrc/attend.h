@@ -9,6 +9,8 @@
 #pragma once
 #include "common.h"
 
+#include <algorithm>
+
 namespace f3m {
 
 // one tensor of rows x heads x head_dim, strides in values
@@ -85,6 +87,11 @@ struct F16 {
         return __builtin_bit_cast(uint32_t, __builtin_amdgcn_cvt_scalef32_pk_f16_fp8(w, scale, HIGH));
     }
 };
+
+// tiles of 128 rows of all groups: `tiles` in the longest sequence, at most as many as all rows make
+inline int64_t all_tiles(const AttendArgs &a, int64_t tiles, int64_t rows) {
+    return std::max<int64_t>(1, std::min(tiles * a.groups, (rows / 128 + a.batch) * a.kv_heads));
+}
 
 // attend.hip, attend_grad.hip: the launches, and the bytes of workspace that they need
 int64_t attend_workspace(AttendArgs a, int64_t max_k);

@@ -654,30 +654,42 @@ template <class T> void launch_dim(const AttendArgs &a, bool e8, bool few, int64
     else e8 ? launch<T, 128, true>(a, few, blocks, st) : launch<T, 128, false>(a, few, blocks, st);
 }
 
-// Up to 64 rows to a key head go to attend_few.  A long key axis is cut into parts where the rows alone make too few blocks: two
-// blocks of attend_many fit a CU (three up to a head size of 64), one of attend_few (two with 8-bit codes), whose waves keep 64 KB or more
-// under way.
+// Up to 64 rows to a key head go to attend_few: with 64 rows of a sequence attend_many would have half of its waves idle.  A long key axis is
+// cut into parts where the rows alone make too few blocks.
+// attend_few: one block to a CU at a time (two with 8-bit codes), whose waves keep 64 KB or more under way; four rounds of blocks, for
+// sequences of different lengths.
+// attend_many: two blocks to a CU (three up to a head size of 64).  Where causal order makes the rows' lengths rise along the sequence, as many
+// parts as fill 88 % of those places, p parts of the longest being about (p + 1) / 2 to a tile (4096 tokens, 8 heads, one key head: 84 us
+// whole, 71 in 2 parts, 64 in 3, 80 in 4); else the fewest rounds for the work of one, a part costing some of it (twice 500 new tokens
+// after 7500, 8 heads, 2 key heads: 183 us whole, 67 in 4 parts, 63 in 8, 75 in 16).  Parts have 8 or 10 tiles or more, since shorter
+// ones cost as much as they save (4 x 1024 tokens, 8 heads of 64, no order: 21 us whole, 33 in two parts).
 bool split(AttendArgs &a, int64_t max_k, bool e8) {
     const bool few = (int64_t)a.max_q * a.group <= 64;
-    const int per = few ? 32 : KT, rows = few ? 32 : 128, least = few ? 16 : 8;
+    const int per = few ? 32 : KT, rows = few ? 32 : 128;
     a.tiles = (int)cdiv((int64_t)a.max_q * a.group, rows);
-    const int64_t most = most_tiles(a, max_k, rows, per), items = (int64_t)a.tiles * a.groups;
-    int64_t parts = 1;
+    const int64_t most = most_tiles(a, max_k, rows, per);
     if (few) {
-        parts = cdiv(e8 ? 2048 : 1024, items);   // four rounds, for sequences of different lengths
-    } else if (const int64_t slots = a.dim > 64 ? 512 : 768; items < slots) {   // the fewest rounds of blocks for the work of one, a part costing some of it
-        double least_cost = 1e30;
-        for (int64_t rounds = 0; rounds <= 6; ++rounds) {   // as many parts as fill them; 0: one part
-            const int64_t p = rounds ? rounds * slots / items : 1;
-            const double cost = (double)cdiv(items * p, slots) / (double)p + 0.02 * (double)p * (double)items / (double)slots;
-            if (cost < least_cost) {
-                least_cost = cost;
-                parts = p;
+        const int64_t parts = cdiv(e8 ? 2048 : 1024, (int64_t)a.tiles * a.groups);
+        a.chunk = (int)std::min(std::max(cdiv(most, parts), std::min<int64_t>(16, most)), (int64_t)PAGES_MAX / 4);
+    } else {
+        const int64_t places = a.dim > 64 ? 512 : 768, items = all_tiles(a, a.tiles, a.total_q * a.group);
+        int64_t parts = 1;
+        if (a.causal && most == cdiv(max_k, per) && 2 * (int64_t)a.max_q >= max_k) {
+            parts = std::min((44 * places / 25 - items / 2) / items, most / 8);
+        } else if (items < places) {
+            double least = 1e30;
+            for (int64_t rounds = 0; rounds <= 6; ++rounds) {   // as many parts as fill them; 0: one part
+                const int64_t p = rounds ? rounds * places / items : 1;
+                const double cost = (double)cdiv(items * p, places) / (double)p + 0.02 * (double)p * (double)items / (double)places;
+                if (cost < least) {
+                    least = cost;
+                    parts = p;
+                }
             }
+            parts = std::min(parts, most / 10);
         }
+        a.chunk = (int)cdiv(most, std::max<int64_t>(1, parts));
     }
-    a.chunk = (int)std::max<int64_t>(cdiv(most, parts), std::min<int64_t>(least, most));
-    if (few) a.chunk = std::min(a.chunk, PAGES_MAX / 4);
     a.parts = (int)cdiv(most, a.chunk);
     return few;
 }

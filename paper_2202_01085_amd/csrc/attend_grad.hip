@@ -507,11 +507,6 @@ template <class T> __global__ __launch_bounds__(NT) void join_keys(AttendArgs a)
     *(u32x2 *)(a.dv.p + 2 * (row * a.dv.row + (int64_t)hk * a.dv.head + x)) = (u32x2){T::pack(v.x, v.y), T::pack(v.z, v.w)};
 }
 
-// tiles of 128 rows of all groups: `tiles` in the longest sequence, at most as many as all rows make
-int64_t all_tiles(const AttendArgs &a, int64_t tiles, int64_t rows) {
-    return std::max<int64_t>(1, std::min(tiles * a.groups, (rows / 128 + a.batch) * a.kv_heads));
-}
-
 // How grad_keys is cut.  A block has a CU to itself at head sizes above 64, half of one below: 256 or 512 places.  Blocks go to the XCDs in
 // turn, whatever their length, so that a little more than one round of them takes as long as two.
 // With a window, without order or with few tokens after many keys, tiles are about equally long (`usual`) but those of the sinks, which
