@@ -654,7 +654,9 @@ template <class T> void launch_dim(const AttendArgs &a, bool e8, bool few, int64
     else e8 ? launch<T, 128, true>(a, few, blocks, st) : launch<T, 128, false>(a, few, blocks, st);
 }
 
-// Up to 64 rows to a key head go to attend_few: with 64 rows of a sequence attend_many would have half of its waves idle.  A long key axis is
+// Up to 32 rows to a key head go to attend_few, one tile of its rows (a token each of 64 sequences of up to 8192, 4 heads to a key head, 8-bit
+// cache: 146 us, 206 in attend_many; of one of 32768: 27 and 31; of 16 of 4096 each: 44 and 40), more to attend_many (64 rows of 16 sequences
+// of 4096: 52 us, 75 in attend_few; of one of 32768: 38 and 42).  A long key axis is
 // cut into parts where the rows alone make too few blocks.
 // attend_few: one block to a CU at a time (two with 8-bit codes), whose waves keep 64 KB or more under way; four rounds of blocks, for
 // sequences of different lengths.
@@ -664,7 +666,7 @@ template <class T> void launch_dim(const AttendArgs &a, bool e8, bool few, int64
 // after 7500, 8 heads, 2 key heads: 183 us whole, 67 in 4 parts, 63 in 8, 75 in 16).  Parts have 8 or 10 tiles or more, since shorter
 // ones cost as much as they save (4 x 1024 tokens, 8 heads of 64, no order: 21 us whole, 33 in two parts).
 bool split(AttendArgs &a, int64_t max_k, bool e8) {
-    const bool few = (int64_t)a.max_q * a.group <= 64;
+    const bool few = (int64_t)a.max_q * a.group <= 32;
     const int per = few ? 32 : KT, rows = few ? 32 : 128;
     a.tiles = (int)cdiv((int64_t)a.max_q * a.group, rows);
     const int64_t most = most_tiles(a, max_k, rows, per);
