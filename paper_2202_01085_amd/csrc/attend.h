@@ -1,4 +1,4 @@
-// Row-normalised products (attention): what the kernels of attend.hip, attend_grad.hip and attend_few.hip share.
+// Row-normalised products (attention): what the kernels of attend.hip, attend_grad.hip and cache.hip share.
 //
 // Every product of a 32 x 32 block runs on v_mfma_f32_32x32x16 (fp32 sums).  Lane l of a wave has the operand values
 //   A[l % 32][8 (l / 32) + j],  B[8 (l / 32) + j][l % 32],  j = 0..7
