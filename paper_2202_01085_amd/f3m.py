@@ -530,16 +530,17 @@ class KVCache:
     def __init__(self, k, v, k_exp=None, v_exp=None):
         if not (isinstance(k, torch.Tensor) and k.is_cuda and k.dim() == 4 and k.dtype in DTYPES):
             raise TypeError("k must be a device tensor (pages, kv_heads, page_size, head_dim) of bfloat16, float16 or float8_e4m3fn")
-        c = CacheInfo(held=DTYPES[k.dtype], pages=k.shape[0], kv_heads=k.shape[1], page_size=k.shape[2], head_dim=k.shape[3])
-        c.k = _device_array(k, "k", k.dtype, k.device, k.shape)
-        c.v = _device_array(v, "v", k.dtype, k.device, k.shape)
-        if k.dtype == torch.float8_e4m3fn:
-            c.k_exp = _device_array(k_exp, "k_exp", torch.uint8, k.device, k.shape[:3])
-            c.v_exp = _device_array(v_exp, "v_exp", torch.uint8, k.device, k.shape[:3])
+        dtype, device, shape = k.dtype, k.device, k.shape
+        at_k, at_v = _device_array(k, "k", dtype, device, shape), _device_array(v, "v", dtype, device, shape)
+        at_k_exp = at_v_exp = None
+        if dtype == torch.float8_e4m3fn:
+            rows = shape[:3]
+            at_k_exp, at_v_exp = _device_array(k_exp, "k_exp", torch.uint8, device, rows), _device_array(v_exp, "v_exp", torch.uint8, device, rows)
         elif k_exp is not None or v_exp is not None:
             raise ValueError("k_exp and v_exp belong to 8-bit caches")
         self.k, self.v, self.k_exp, self.v_exp = k, v, k_exp, v_exp
-        self._c = c
+        pages, heads, page_size, dim = shape
+        self._c = CacheInfo(DTYPES[dtype], heads, dim, page_size, pages, at_k, at_v, at_k_exp, at_v_exp)
 
     @classmethod
     def empty(cls, pages, page_size, kv_heads, head_dim, dtype=torch.float8_e4m3fn, device="cuda"):
