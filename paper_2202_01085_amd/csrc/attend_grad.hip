@@ -8,7 +8,7 @@
 // a power of two per kept row or key that goes down when a larger one comes, so both keep 11 bits.
 //
 // Bound by the matrix cores and LDS, at head size 64 by vector issue.  4 x 2048 tokens with causal order, 16 heads of 128, 4 key heads: rows
-// 117 us (0.88 PFLOP/s in three products), keys 160 to 170 (0.8 in four), sums of parts 9; 8192 tokens in a window of 1024, heads of 64: rows
+// 119 us (0.87 PFLOP/s in three products), keys 172 (0.8 in four), sums of parts 8; 8192 tokens in a window of 1024, heads of 64: rows
 // 68, keys 118.
 #include "attend.h"
 
