@@ -666,8 +666,12 @@ template <class T> void launch_dim(const AttendArgs &a, bool e8, bool few, int64
 // cache: 146 us, 206 in attend_many; of one of 32768: 27 and 31; of 16 of 4096 each: 44 and 40), more to attend_many (64 rows of 16 sequences
 // of 4096: 52 us, 75 in attend_few; of one of 32768: 38 and 42).  A long key axis is
 // cut into parts where the rows alone make too few blocks.
-// attend_few: one block to a CU at a time (two with 8-bit codes), whose waves keep 64 KB or more under way; four rounds of blocks, for
-// sequences of different lengths.
+// attend_few: one block to a CU at a time (two with 8-bit codes), whose waves keep 64 KB or more under way; as many parts as fill one round of
+// them (one token after 131071 in 16 bits, 8 key heads: 112 us in 8 parts, 102 in 32, 109 in 64, 119 in 128; 16 sequences of 4096 in 8
+// bits: 55 us whole, 35 in 4 parts, 44 in 8).  Where that leaves one, three in 8 bits from 4096 keys on, since sequences differ in length (64
+// of up to 8192: 153 us whole, 137 in 3; all as long as the longest: 203 and 213; 64 of up to 1000: 28 and 43), in 16 bits it stays
+// (24 of up to 6000: 87 and 84; all as long: 106 and 132).
+// Up to 512 keys the second launch costs more than it saves.
 // attend_many: two blocks to a CU (three up to a head size of 64).  Where causal order makes the rows' lengths rise along the sequence, as many
 // parts as fill 88 % of those places, p parts of the longest being about (p + 1) / 2 to a tile (4096 tokens, 8 heads, one key head: 84 us
 // whole, 71 in 2 parts, 64 in 3, 80 in 4); else the fewest rounds for the work of one, a part costing some of it (twice 500 new tokens
@@ -679,8 +683,9 @@ bool split(AttendArgs &a, int64_t max_k, bool e8) {
     a.tiles = (int)cdiv((int64_t)a.max_q * a.group, rows);
     const int64_t most = most_tiles(a, max_k, rows, per);
     if (few) {
-        const int64_t parts = cdiv(e8 ? 2048 : 1024, (int64_t)a.tiles * a.groups);
-        a.chunk = (int)std::min(std::max(cdiv(most, parts), std::min<int64_t>(16, most)), (int64_t)PAGES_MAX / 4);
+        int64_t parts = (e8 ? 512 : 256) / ((int64_t)a.tiles * a.groups);
+        if (parts <= 1) parts = e8 && most >= 128 ? 3 : 1;
+        a.chunk = (int)std::min(most > 16 ? std::max<int64_t>(cdiv(most, parts), 4) : most, (int64_t)PAGES_MAX / 4);
     } else {
         const int64_t places = a.dim > 64 ? 512 : 768, items = all_tiles(a, a.tiles, a.total_q * a.group);
         int64_t parts = 1;
