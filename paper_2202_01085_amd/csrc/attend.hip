@@ -353,8 +353,8 @@ template <class T, int DP, bool E8> __global__ __launch_bounds__(NT, DP == 128 ?
 
 // Few rows (single tokens, short chunks): a work item is 32 rows and a part of the keys; each of the four waves takes every fourth
 // tile of 32 keys through a ring in LDS of its own, and the four results are joined at the end.  Bound by the reading of K and V: a token each
-// of 64 sequences of up to 8192, 8 key heads of 128 in 8 bits: 140 us, 4.2 TB/s; one token after 131071 in 16 bits: 117 us with the join,
-// 4.6 TB/s (a copy reaches 4.7).
+// of 64 sequences of up to 8192, 8 key heads of 128 in 8 bits: 136 us, 4.4 TB/s; one token after 131071 in 16 bits: 102 us with the join,
+// 5.3 TB/s (a copy reaches 4.7, reading and writing; some of it comes from the last-level cache).
 constexpr int PAGES_MAX = 1024;   // page numbers of a work item
 
 template <class T, int DP, bool E8> __global__ __launch_bounds__(NT, E8 ? 2 : 1) void attend_few(AttendArgs a) {
