@@ -286,16 +286,17 @@ __device__ __forceinline__ u32x4 buffer_of(const char *p, int bytes) {   // read
 constexpr uint32_t NOWHERE = 0xffffff00u;   // an offset past every buffer
 // What the hardware asks for and the compiler sees to in its own code, but not inside an asm: a wait state between the write of m0 and the load
 // that reads it; five between a vector instruction that writes a scalar register (a v_readfirstlane for the buffer or the offset, which the
-// compiler may put right before) and a memory instruction that reads it: s_mov is one, s_nop 3 four.
+// compiler may put right before) and a memory instruction that reads it: s_mov is one, s_nop 3 four.  m0 is reserved and cannot be named as
+// written; the compiler keeps nothing in it, and uses it for nothing else here.
 __device__ __forceinline__ void to_lds(u32x4 buffer, uint32_t lane_offset, uint32_t offset, uint32_t lds) {
     asm volatile("s_mov_b32 m0, %0\n\ts_nop 3\n\tbuffer_load_dwordx4 %1, %2, %3 offen lds" ::"s"(__builtin_amdgcn_readfirstlane(lds)), "v"(lane_offset),
-                 "s"(buffer), "s"(__builtin_amdgcn_readfirstlane(offset)) : "memory", "m0");
+                 "s"(buffer), "s"(__builtin_amdgcn_readfirstlane(offset)) : "memory");
 }
 __device__ __forceinline__ void to_lds(const char *p, uint32_t lds) {
-    asm volatile("s_mov_b32 m0, %0\n\ts_nop 0\n\tglobal_load_lds_dwordx4 %1, off" ::"s"(__builtin_amdgcn_readfirstlane(lds)), "v"(p) : "memory", "m0");
+    asm volatile("s_mov_b32 m0, %0\n\ts_nop 0\n\tglobal_load_lds_dwordx4 %1, off" ::"s"(__builtin_amdgcn_readfirstlane(lds)), "v"(p) : "memory");
 }
 __device__ __forceinline__ void word_to_lds(const float *p, uint32_t lds) {   // 4 bytes to a lane
-    asm volatile("s_mov_b32 m0, %0\n\ts_nop 0\n\tglobal_load_lds_dword %1, off" ::"s"(__builtin_amdgcn_readfirstlane(lds)), "v"(p) : "memory", "m0");
+    asm volatile("s_mov_b32 m0, %0\n\ts_nop 0\n\tglobal_load_lds_dword %1, off" ::"s"(__builtin_amdgcn_readfirstlane(lds)), "v"(p) : "memory");
 }
 // waits until at most LEFT of the wave's loads are under way (they arrive in the order of their issue)
 template <int LEFT = 0> __device__ __forceinline__ void arrived() { asm volatile("s_waitcnt vmcnt(%0)" ::"i"(LEFT) : "memory"); }
