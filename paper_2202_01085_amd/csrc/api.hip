@@ -60,7 +60,8 @@ void copy_to_host(T *dst, const T *src, size_t count) {
 
 // ---- attention ----
 
-f3m::Rows rows_of(const f3m_rows &r) { return {(char *)r.data, r.row, r.head}; }
+// the stride of one row alone means nothing and may be any number: the kernels compute with strides below 2^22
+f3m::Rows rows_of(const f3m_rows &r, int64_t rows, int dim) { return {(char *)r.data, rows > 1 ? r.row : dim, r.head}; }
 
 // `paged`: k, v, k_offsets and total_k are not read
 f3m_status check_attention(const f3m_attention_args *p, bool paged = false) {
@@ -158,9 +159,9 @@ f3m::AttendArgs attend_args(const f3m_attention_args &p) {
     a.max_q = (int)std::min<int64_t>(p.max_q, p.total_q);
     a.q_offsets = p.q_offsets;
     a.k_offsets = p.k_offsets;
-    a.q = rows_of(p.q);
-    a.k = rows_of(p.k);
-    a.v = rows_of(p.v);
+    a.q = rows_of(p.q, p.total_q, p.head_dim);
+    a.k = rows_of(p.k, p.total_k, p.head_dim);
+    a.v = rows_of(p.v, p.total_k, p.head_dim);
     a.groups = p.batch * p.kv_heads;
     return a;
 }
@@ -374,7 +375,7 @@ f3m_status f3m_attention(const f3m_attention_args *args, const f3m_rows *out, fl
     f3m::AttendArgs a = attend_args(*args);
     st = check_workspace(workspace, workspace_bytes, f3m::attend_workspace(a, args->max_k));
     if (st != F3M_OK) return st;
-    a.out = rows_of(*out);
+    a.out = rows_of(*out, args->total_q, args->head_dim);
     a.lse = lse;
     return guarded([&] { f3m::run_attend(a, args->max_k, args->dtype == F3M_F16, false, workspace, (hipStream_t)stream); });
 }
@@ -402,14 +403,14 @@ f3m_status f3m_attention_grad(const f3m_attention_args *args, const f3m_rows *do
     st = check_workspace(workspace, workspace_bytes, f3m::attend_grad_workspace(a, args->max_k));
     if (st != F3M_OK) return st;
     if (args->total_q > 0) {
-        a.dout = rows_of(*dout);
-        a.out = rows_of(*out);
+        a.dout = rows_of(*dout, args->total_q, args->head_dim);
+        a.out = rows_of(*out, args->total_q, args->head_dim);
         a.lse = const_cast<float *>(lse);
-        a.dq = rows_of(*dq);
+        a.dq = rows_of(*dq, args->total_q, args->head_dim);
     }
     if (args->total_k > 0) {
-        a.dk = rows_of(*dk);
-        a.dv = rows_of(*dv);
+        a.dk = rows_of(*dk, args->total_k, args->head_dim);
+        a.dv = rows_of(*dv, args->total_k, args->head_dim);
     }
     return guarded([&] { f3m::run_attend_grad(a, args->max_k, args->dtype == F3M_F16, workspace, (hipStream_t)stream); });
 }
@@ -453,7 +454,7 @@ f3m_status f3m_cache_attention(const f3m_cache *cache, const f3m_attention_args 
     f3m::AttendArgs a = attend_args(*args);
     st = check_workspace(workspace, workspace_bytes, f3m::attend_workspace(a, args->max_k));
     if (st != F3M_OK) return st;
-    a.out = rows_of(*out);
+    a.out = rows_of(*out, args->total_q, args->head_dim);
     a.lse = lse;
     a.k = {(char *)cache->k, 0, 0};
     a.v = {(char *)cache->v, 0, 0};

@@ -283,14 +283,13 @@ __device__ __forceinline__ u32x4 buffer_of(const char *p, int bytes) {   // read
     return (u32x4){(uint32_t)__builtin_amdgcn_readfirstlane((uint32_t)at), (uint32_t)__builtin_amdgcn_readfirstlane((uint32_t)(at >> 32)),
                    (uint32_t)__builtin_amdgcn_readfirstlane((uint32_t)bytes), 0x00020000u};
 }
-constexpr uint32_t NOWHERE = 0xffffff00u;   // an offset past every buffer
+constexpr uint32_t NOWHERE = 0x80000000u;   // an offset past every buffer, also with the rows of a tile (64 x 2^23 bytes) added to it
 // What the hardware asks for and the compiler sees to in its own code, but not inside an asm: a wait state between the write of m0 and the load
-// that reads it; five between a vector instruction that writes a scalar register (a v_readfirstlane for the buffer or the offset, which the
-// compiler may put right before) and a memory instruction that reads it: s_mov is one, s_nop 3 four.  m0 is reserved and cannot be named as
-// written; the compiler keeps nothing in it, and uses it for nothing else here.
-__device__ __forceinline__ void to_lds(u32x4 buffer, uint32_t lane_offset, uint32_t offset, uint32_t lds) {
-    asm volatile("s_mov_b32 m0, %0\n\ts_nop 3\n\tbuffer_load_dwordx4 %1, %2, %3 offen lds" ::"s"(__builtin_amdgcn_readfirstlane(lds)), "v"(lane_offset),
-                 "s"(buffer), "s"(__builtin_amdgcn_readfirstlane(offset)) : "memory");
+// that reads it; five between a vector instruction that writes a scalar register (a v_readfirstlane for the buffer, which the compiler may
+// put right before) and a memory instruction that reads it: s_mov is one, s_nop 3 four.
+__device__ __forceinline__ void to_lds(u32x4 buffer, uint32_t lane_offset, uint32_t lds) {
+    asm volatile("s_mov_b32 m0, %0\n\ts_nop 3\n\tbuffer_load_dwordx4 %1, %2, 0 offen lds" ::"s"(__builtin_amdgcn_readfirstlane(lds)), "v"(lane_offset),
+                 "s"(buffer) : "memory");
 }
 __device__ __forceinline__ void to_lds(const char *p, uint32_t lds) {
     asm volatile("s_mov_b32 m0, %0\n\ts_nop 0\n\tglobal_load_lds_dwordx4 %1, off" ::"s"(__builtin_amdgcn_readfirstlane(lds)), "v"(p) : "memory");
@@ -326,10 +325,13 @@ template <class T, int DP, int N, int WAVES = 4> struct Tile2 {
     // rows from row0 on of one tensor; rows from `end` on give zeros
     template <int W> __device__ void issue_one(int row0, int end, int dim, const short *tile, int wave) const {
         if (N < STEP && wave * RPI >= N) return;
-        const u32x4 buffer = buffer_of(base[W] + (int64_t)row0 * stride[W], (min(end - row0, N) - 1) * stride[W] + 2 * dim);
+        const char *const at = base[W] + (int64_t)row0 * stride[W];
+        const int bytes = (min(end - row0, N) - 1) * stride[W] + 2 * dim;
         const uint32_t lds = lds_address(tile) + wave * 1024;
+        const u32x4 buffer = buffer_of(at, bytes);
+        // the whole offset in the lane's register: that is what is checked against the buffer's bytes
 #pragma unroll
-        for (int c = 0; c < COUNT; ++c) to_lds(buffer, off[W], (uint32_t)(STEP * c * stride[W]), lds + 1024 * WAVES * c);
+        for (int c = 0; c < COUNT; ++c) to_lds(buffer, off[W] + (uint32_t)(STEP * c * stride[W]), lds + 1024 * WAVES * c);
     }
     __device__ void issue(int row0, int end, int dim, const short *tx, const short *ty, int wave) const {
         issue_one<0>(row0, end, dim, tx, wave);

@@ -1,0 +1,70 @@
+"""f3m.attention, its gradients and the cache where rows that do not count lie next to rows that do: what those hold (NaN) reaches nobody, and
+every row that counts is computed.  Against the definition in 64 bits (attention_util.py, with the tolerances)."""
+import ctypes
+
+import numpy as np
+import pytest
+import torch
+
+import attention_util as au
+from paper_2202_01085_amd import f3m
+
+pytestmark = pytest.mark.gpu
+DEV = "cuda:0"
+BF, HF, E8 = torch.bfloat16, torch.float16, torch.float8_e4m3fn
+NAN = float("nan")
+
+
+def normal(shape, seed, type, size=1.0):
+    g = torch.Generator().manual_seed(seed)
+    return (torch.randn(shape, generator=g) * size).to(type)
+
+
+def dev_offsets(o):
+    return torch.tensor(o, dtype=torch.int32, device=DEV)
+
+
+@pytest.mark.parametrize("type", [BF, HF])
+@pytest.mark.parametrize("D", [32, 64, 80, 128])
+@pytest.mark.parametrize("how", [{}, dict(causal=False), dict(window=9, sinks=2)])
+def test_short_sequences_between_neighbours_of_nan(type, D, how):
+    """sequences that end inside a tile, each followed by one whose q, k, v and dout are NaN: what a tile would hold of the neighbour is zeros"""
+    lengths = [5, 70, 20, 3, 40, 64, 33, 1, 97, 130, 1, 66]
+    off = au.offsets(lengths)
+    q, k, v, do = (normal((off[-1], h, D), 70 + i, type) for i, h in enumerate((4, 2, 2, 4)))
+    clean = torch.zeros(off[-1], dtype=torch.bool)
+    for b in range(0, len(lengths), 2):
+        clean[off[b]:off[b + 1]] = True
+    want = au.batch(q, k, v, off, off, 0.125, dout=do, **how)
+    for x in (q, k, v, do):
+        x[~clean] = NAN
+    print("neighbours", type, D, how, flush=True)
+    q, k, v, do = (x.to(DEV) for x in (q, k, v, do))
+    at = dev_offsets(off)
+    call = dict(q_offsets=at, k_offsets=at, max_q=130, max_k=130, scale=0.125, **how)
+    out, lse = f3m.attention(q, k, v, **call)
+    got = dict(zip(("dq", "dk", "dv"), f3m.attention_grad(do, q, k, v, out, lse, **call)), out=out, lse=lse)
+    for name, x in got.items():
+        au.close(x[clean.to(DEV)], {n: want[n][clean] for n in (name, name + "_tol")}, name)
+        assert torch.isnan(x[~clean.to(DEV)]).any()
+
+
+def test_a_stride_of_one_row_means_nothing():
+    """tensors of one row through the C entries, with strides between rows that no tensor has"""
+    D, stream = 80, torch.cuda.current_stream().cuda_stream
+    q, k, v, do = (normal((1, h, D), 80 + i, BF) for i, h in enumerate((2, 1, 1, 2)))
+    want = au.batch(q, k, v, [0, 1], [0, 1], 0.125, dout=do)
+    dev = {n: x.to(DEV) for n, x in dict(q=q, k=k, v=v, dout=do).items()}
+    for row in (0, 8, 1 << 22, (1 << 31) - 8, (1 << 32) + 8, 1 << 40):
+        a = f3m.AttentionArgs(dtype=0, batch=1, heads=2, kv_heads=1, head_dim=D, causal=1, scale=0.125, max_q=1, max_k=1, total_q=1, total_k=1)
+        a.q, a.k, a.v, g = (f3m.Rows(dev[n].data_ptr(), row, D) for n in ("q", "k", "v", "dout"))
+        got = {n: torch.full_like(dev[x], 7.0) for n, x in (("out", "q"), ("dq", "q"), ("dk", "k"), ("dv", "v"))}
+        got["lse"] = torch.full((1, 2), 7.0, device=DEV)
+        o, dq, dk, dv = (f3m.Rows(got[n].data_ptr(), row, D) for n in ("out", "dq", "dk", "dv"))
+        need = max(f3m.lib().f3m_attention_workspace(ctypes.byref(a)), f3m.lib().f3m_attention_grad_workspace(ctypes.byref(a)))
+        w = torch.empty(need, dtype=torch.uint8, device=DEV)
+        assert f3m.lib().f3m_attention(ctypes.byref(a), ctypes.byref(o), got["lse"].data_ptr(), w.data_ptr(), need, stream) == 0
+        assert f3m.lib().f3m_attention_grad(ctypes.byref(a), ctypes.byref(g), ctypes.byref(o), got["lse"].data_ptr(), ctypes.byref(dq), ctypes.byref(dk),
+                                            ctypes.byref(dv), w.data_ptr(), need, stream) == 0
+        for name, x in got.items():
+            au.close(x, want, name)

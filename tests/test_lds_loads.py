@@ -12,8 +12,8 @@ extern "C" __global__ void probe(const char *p, const int *from, int stride, flo
     __shared__ __attribute__((aligned(1024))) short t[8192];
     const int w = from[threadIdx.x], x = from[threadIdx.x + 64], y = from[threadIdx.x + 128];
     const u32x4 buffer = buffer_of(p + w, x);
-    to_lds(buffer, 16 * threadIdx.x, y, lds_address(t) + 1024 * (w & 1));
-    to_lds(buffer, 16 * threadIdx.x, y + stride, lds_address(t) + 1024 * (x & 1));
+    to_lds(buffer, 16 * threadIdx.x, lds_address(t) + 1024 * (w & 1));
+    to_lds(buffer, 16 * threadIdx.x + stride, lds_address(t) + 1024 * (x & 1));
     to_lds(p + 16 * threadIdx.x, lds_address(t) + 1024 * (y & 1));
     word_to_lds((const float *)p + threadIdx.x, lds_address(t) + 1024 * (from[threadIdx.x + 192] & 1));
     arrived();
@@ -77,8 +77,11 @@ def test_waits_before_loads_to_lds(tmp_path):
     res = subprocess.run([build._hipcc(), *build.FLAGS, "-I", build.CSRC, "-S", "--cuda-device-only", src, "-o", out], capture_output=True, text=True)
     assert res.returncode == 0, res.stderr
     with open(out) as f:
-        loads, faults = check(f.read())
+        text = f.read()
+    loads, faults = check(text)
     assert loads == 4 and not faults, faults
+    # what is checked against the buffer's bytes is the lane's offset: all of it stands there, none in a scalar register
+    assert re.findall(r"buffer_load_dwordx4 v\d+, s\[\d+:\d+\], (\S+) offen lds", text) == ["0", "0"]
 
 
 def test_no_other_way_to_lds():
