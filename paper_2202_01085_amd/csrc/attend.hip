@@ -281,7 +281,7 @@ template <class T, int DP, bool E8> __global__ __launch_bounds__(NT, DP == 128 ?
                 if (t + 1 < end) next.look(a, s, b, tiles[t + 1] * KT, tid);
             };
             auto keep = [&](int t, int buf) {
-                const uint64_t odd = next.store(tile[buf][0], tile[buf][1], tid, careful && !whole(tiles[t] * KT));
+                const uint64_t odd = next.store(tile[buf][0], tile[buf][1], tid, careful && (!whole(tiles[t] * KT) || good != ~0ull));
                 if (careful && lane == 0) odd_rows[buf][wave] = odd;
                 if (tid == 0) good_rows[buf] = good;
             };

@@ -68,3 +68,44 @@ def test_a_stride_of_one_row_means_nothing():
                                             ctypes.byref(dv), w.data_ptr(), need, stream) == 0
         for name, x in got.items():
             au.close(x, want, name)
+
+
+def paged(type, held, lengths, heads, D, page, seed):
+    """a cache whose page 0 and free rows are NaN, sequences in shuffled pages other than 0; the table, the packed keys and values that it holds"""
+    counts = [-(-n // page) for n in lengths]
+    order = torch.randperm(sum(counts), generator=torch.Generator().manual_seed(seed)) + 1
+    c = f3m.KVCache.empty(sum(counts) + 1, page, heads, D, dtype=held, device=DEV)
+    for x in (c.k, c.v):
+        (x.view(torch.uint8) if held == E8 else x).fill_(0x7f if held == E8 else NAN)
+    table = torch.full((len(lengths), max(counts)), -1, dtype=torch.int32)
+    slots, at = [], 0
+    for b, n in enumerate(lengths):
+        table[b, :counts[b]] = order[at:at + counts[b]].int()
+        at += counts[b]
+        j = torch.arange(n)
+        slots.append(table[b, j // page].long() * page + j % page)
+    slots = torch.cat(slots).to(DEV)
+    k, v = (normal((sum(lengths), heads, D), seed + i, type) for i in (1, 2))
+    c.write(k.to(DEV), v.to(DEV), slots)
+    return (c, table) + tuple(x.cpu() for x in c.read(slots, dtype=type))
+
+
+@pytest.mark.parametrize("type,held", [(BF, E8), (HF, E8), (BF, BF), (HF, HF)])
+@pytest.mark.parametrize("D,page,new", [(64, 16, 70), (128, 32, 40), (32, 8, 200), (128, 128, 33), (64, 16, 3)])
+def test_bad_pages_in_tiles_that_the_mask_leaves_whole(type, held, D, page, new):
+    """page numbers outside the cache in the middle of what all tokens see; page 0, which no sequence has, is NaN"""
+    n = 700
+    c, table, k, v = paged(type, held, [n], 1, D, page, D + page)
+    hidden = [128 // page, 300 // page]
+    table[0, hidden[0]], table[0, hidden[1]] = -7, 10 ** 9
+    keep = torch.ones(n, dtype=torch.bool)
+    for x in hidden:
+        keep[x * page:(x + 1) * page] = False
+    q = normal((new, 2, D), 4, type)
+    print("bad pages", type, held, D, page, new, flush=True)
+    out, lse = c.attention(q.to(DEV), table.to(DEV), torch.tensor([n], dtype=torch.int32, device=DEV), scale=0.125)
+    u, narrow = torch.finfo(type).eps / 2, type == HF
+    for h in range(2):
+        r = au.sequence(q[:, h].double(), k[:, 0].double(), v[:, 0].double(), au.visible(new, n, True, 0, 0) & keep, 0.125, u, narrow)
+        au.close(out[:, h], r, "out")
+        au.close(lse[:, h], r, "lse")
