@@ -561,7 +561,8 @@ __device__ __forceinline__ bool in_sequence(const AttendArgs &a, int64_t token) 
         if (a.q_offsets[mid + 1] <= token) lo = mid + 1;
         else hi = mid;
     }
-    return lo < a.batch && token >= a.q_offsets[lo] && token - a.q_offsets[lo] < a.max_q;
+    const int64_t first = max(lo < a.batch ? a.q_offsets[lo] : 0, 0);      // as sequence_of cuts it
+    return lo < a.batch && token >= first && token - first < a.max_q;
 }
 template <class T> __device__ __forceinline__ void store_joined(const AttendArgs &a, int64_t row, int x, float top, float sum, float4 o) {
     const float by = sum > 0.f ? 1.f / sum : sum == sum ? 0.f : sum;

@@ -109,3 +109,15 @@ def test_bad_pages_in_tiles_that_the_mask_leaves_whole(type, held, D, page, new)
         r = au.sequence(q[:, h].double(), k[:, 0].double(), v[:, 0].double(), au.visible(new, n, True, 0, 0) & keep, 0.125, u, narrow)
         au.close(out[:, h], r, "out")
         au.close(lse[:, h], r, "lse")
+
+
+@pytest.mark.parametrize("nq,nk,group", [(20, 9000, 1), (1, 9000, 8), (90, 9000, 2), (600, 300, 1)])
+@pytest.mark.parametrize("first", [-5, -100000])
+def test_a_first_offset_below_zero_is_cut_to_zero(nq, nk, group, first):
+    """every row counts, also where the call works in parts (the first three) and where it does not"""
+    q, k, v = normal((nq, group, 64), 1, BF), normal((nk, 1, 64), 2, BF), normal((nk, 1, 64), 3, BF)
+    want = au.batch(q, k, v, [0, nq], [0, nk], 0.125)
+    out, lse = torch.full((nq, group, 64), 7.0, dtype=BF, device=DEV), torch.full((nq, group), 7.0, device=DEV)
+    f3m.attention(q.to(DEV), k.to(DEV), v.to(DEV), dev_offsets([first, nq]), dev_offsets([first, nk]), scale=0.125, out=out, lse=lse)
+    au.close(out, want, "out")
+    au.close(lse, want, "lse")
