@@ -36,11 +36,15 @@ struct AttendArgs {
     // the launch
     int tiles, groups, pinned, chunk;         // row tiles of the longest sequence, batch * kv_heads, see block_of, key tiles of a part
     int parts;                                // parts of the key axis; above 1 the results go to part_out, part_lse
-    float *part_out, *part_lse;               // (parts, rows of q, heads, dim) and (parts, rows of q, heads)
+    float *part_out, *part_lse;               // (parts, rows of q, heads, dim) and (parts, rows of q, heads); gradients: see tile_slot
     // gradient
     Rows dout, dq, dk, dv;
     float *stat;                              // (2, heads, rows of q): -log2 of the row's sum (-inf: empty row), -dO.O
-    int split, usual;                         // key tiles of a group that may be cut into parts, chunk row tiles each; parts of tiles without sinks
+    int usual;                                // parts of key tiles without sinks, chunk row tiles each; `parts` is the most of any
+    int sink_tiles, sink_chunk, sink_parts;   // the first key tiles of a sequence, with sinks; row tiles of a part of theirs; the most parts of one
+    int packed, sink_packed;                  // how the parts' sums are numbered, see tile_slot and key_sums
+    int64_t slots, sink_slots;                // numbers of a key head
+    float *sink_out;                          // sums of the sinks' tiles: (sink_slots, sink_tiles, kv_heads, 2, 128, dim)
 };
 
 using s16x4 = __attribute__((ext_vector_type(4))) short;

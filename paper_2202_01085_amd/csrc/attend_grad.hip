@@ -52,6 +52,24 @@ constexpr float LEAST_UNIT = 0x1p-100f;
 // Parts of a tile of `count` steps: `chunk` each, the last one what is left
 __device__ __forceinline__ int parts_of(int count, int chunk, int most) { return min(max(count - 1, 0) / chunk + 1, most); }
 
+// Where the parts' sums lie: by a number of the tile (of 128 rows, `rows` to a token, or keys) among those of all sequences of a key head.  The
+// tiles of sequence b, whose first token is `first`, are numbered from rows first / 128 + b on: the next sequence's start as many further as
+// b has tiles, or more.  Where that makes more numbers than there are tiles of the longest sequence times sequences, those are counted instead.
+__device__ __forceinline__ int64_t tile_slot(const AttendArgs &a, int b, int64_t first, int rows) {
+    return a.packed ? first * rows / 128 + b : (int64_t)b * a.tiles;
+}
+// The sequence that a number belongs to, if to any: the last that starts at or before it
+__device__ __forceinline__ int slot_sequence(const AttendArgs &a, int slot, const int *offsets, int64_t total, int rows) {
+    if (!a.packed) return slot / a.tiles;
+    int lo = 0, hi = a.batch - 1;
+    while (lo < hi) {
+        const int mid = (lo + hi + 1) / 2;
+        if (tile_slot(a, mid, min(max((int64_t)offsets[mid], (int64_t)0), total), rows) <= slot) lo = mid;
+        else hi = mid - 1;
+    }
+    return lo;
+}
+
 // dQ: 128 rows of one group to a block, 32 to a wave, tiles of 64 keys through LDS, as the forward kernel.  Few row tiles are cut into parts
 // along the keys (cut_rows), whose fp32 sums join_rows adds up.  It also leaves each row's
 // stat for grad_keys: -log2 of its sum (+ LIFT), or -inf for an empty row, so that its weights are 0, and -dO.O.
@@ -198,7 +216,8 @@ template <class T, int DP> __global__ __launch_bounds__(NT, 2) void grad_rows(At
     const float by = T::narrow ? a.scale * unit.u : a.scale;
     if (parts > 1) {     // fp32 sums of this part, for join_rows
         if (!valid) return;
-        float *to_part = a.part_out + ((((int64_t)it.group * a.tiles + it.tile) * a.parts + it.part) * 128 + 32 * wave + (lane & 31)) * a.dim;
+        const int64_t at_part = ((tile_slot(a, b, s.q0, a.group) + it.tile) * a.kv_heads + hk) * a.parts + it.part;
+        float *to_part = a.part_out + (at_part * 128 + 32 * wave + (lane & 31)) * a.dim;
 #pragma unroll
         for (int db = 0; db < DB; ++db)
 #pragma unroll
@@ -213,14 +232,15 @@ template <class T, int DP> __global__ __launch_bounds__(NT, 2) void grad_rows(At
 
 // the parts of the row tiles that were cut, summed in their order: a block to 8 rows of a tile, 32 lanes to a row, 4 values each
 template <class T> __global__ __launch_bounds__(NT) void join_rows(AttendArgs a) {
-    const int group = blockIdx.x / (16 * a.tiles), at_tile = blockIdx.x / 16 % a.tiles, in = blockIdx.x % 16 * 8 + threadIdx.x / 32, x = threadIdx.x % 32 * 4;
-    const int b = group / a.kv_heads, hk = group % a.kv_heads, r0 = at_tile * 128;
+    const int in = blockIdx.x % 16 * 8 + threadIdx.x / 32, x = threadIdx.x % 32 * 4, hk = blockIdx.x / 16 % a.kv_heads, slot = blockIdx.x / (16 * a.kv_heads);
+    const int b = slot_sequence(a, slot, a.q_offsets, a.total_q, a.group);
     const Sequence s = sequence_of(a, b);
-    const int rows = min(s.nq, a.max_q) * a.group;
-    if (r0 + in >= rows || x >= a.dim) return;
+    const int at_tile = (int)(slot - tile_slot(a, b, s.q0, a.group)), rows = min(s.nq, a.max_q) * a.group;
+    if (at_tile < 0 || (int64_t)at_tile * 128 + in >= rows || x >= a.dim) return;
+    const int r0 = at_tile * 128;
     const int parts = parts_of(tiles_of<64>(limits_of(a, s, r0 / a.group), limits_of(a, s, min(r0 + 127, rows - 1) / a.group), a.sinks).count, a.chunk, a.parts);
     if (parts == 1) return;
-    const float *from = a.part_out + ((((int64_t)group * a.tiles + at_tile) * a.parts) * 128 + in) * a.dim + x;
+    const float *from = a.part_out + (((int64_t)slot * a.kv_heads + hk) * a.parts * 128 + in) * a.dim + x;
     float4 q = make_float4(0.f, 0.f, 0.f, 0.f);
     for (int p = 0; p < parts; ++p, from += (int64_t)128 * a.dim) {
         const float4 y = *(const float4 *)from;
@@ -251,9 +271,25 @@ __device__ __forceinline__ KeyTile key_tile(const AttendArgs &a, const Sequence 
     return t;
 }
 
-// parts of a key tile
+// row tiles of a part of a key tile, and how many parts it has
+__device__ __forceinline__ int key_chunk(const AttendArgs &a, int at_tile) { return at_tile < a.sink_tiles ? a.sink_chunk : a.chunk; }
 __device__ __forceinline__ int key_parts(const AttendArgs &a, int at_tile, int count) {
-    return at_tile < a.split ? parts_of(count, a.chunk, at_tile < (a.sinks + 127) / 128 ? a.parts : a.usual) : 1;
+    return parts_of(count, key_chunk(a, at_tile), at_tile < a.sink_tiles ? a.sink_parts : a.usual);
+}
+// Where the sums of part 0 of a key tile lie (dk of its 128 keys, dv of them behind those), and how much further those of the
+// next part.  Tiles of sinks, which have parts by the length of their sequence, lie apart.  Sequence b has at most ceil(T group / chunk) of them,
+// T the row tiles of a head, which do not reach past the next sequence's start: T <= end / RT - first / RT + 1.
+struct KeySums {
+    float *at;
+    int64_t next;
+};
+__device__ __forceinline__ KeySums key_sums(const AttendArgs &a, const Sequence &s, int b, int hk, int at_tile) {
+    const int64_t tile = (int64_t)256 * a.dim;
+    if (at_tile < a.sink_tiles) {
+        const int64_t slot = a.sink_packed ? ((int64_t)(s.q0 / RT) + b) * a.group / a.sink_chunk + b : (int64_t)b * a.sink_parts;
+        return {a.sink_out + ((slot * a.sink_tiles + at_tile) * a.kv_heads + hk) * tile, (int64_t)a.sink_tiles * a.kv_heads * tile};
+    }
+    return {a.part_out + ((tile_slot(a, b, s.k0, 1) + at_tile) * a.kv_heads + hk) * a.usual * tile, tile};
 }
 
 // dK, dV: 32 keys to a wave, whose sums stay in registers; tiles of q and dO come through a ring in LDS, two or more under way while one
@@ -278,7 +314,7 @@ template <class T, int DP> __global__ __launch_bounds__(DP == 128 ? 512 : 256, 2
         const int x = (it.part - a.usual) * a.tiles + at_tile, more = a.parts - a.usual;
         at_tile = x / more;
         it.part = a.usual + x % more;
-        if (at_tile >= (a.sinks + 127) / 128) return;
+        if (at_tile >= a.sink_tiles) return;
     }
     const int k0 = at_tile * 128;
     if (k0 >= s.nk) return;
@@ -287,7 +323,7 @@ template <class T, int DP> __global__ __launch_bounds__(DP == 128 ? 512 : 256, 2
     const KeyTile t = key_tile(a, s, k0, min(k0 + 128, s.nk));
     const int parts = key_parts(a, at_tile, t.count);
     if (it.part >= parts) return;
-    const int begin = it.part * a.chunk, end = it.part + 1 < parts ? begin + a.chunk : t.count;
+    const int chunk = key_chunk(a, at_tile), begin = it.part * chunk, end = it.part + 1 < parts ? begin + chunk : t.count;
 
     const int w0 = k0 + 32 * kw, key = w0 + (lane & 31), kept = min(key, s.nk - 1);
     const bool valid = key < s.nk, idle = w0 >= s.nk;
@@ -474,7 +510,8 @@ template <class T, int DP> __global__ __launch_bounds__(DP == 128 ? 512 : 256, 2
     }
     const int64_t row = s.k0 + kept;
     if (parts > 1) {     // fp32 sums of this part, for join_keys
-        float *to_part = a.part_out + ((((int64_t)it.group * a.split + at_tile) * a.parts + it.part) * 256 + 32 * kw + (lane & 31)) * a.dim;
+        const KeySums sums = key_sums(a, s, b, hk, at_tile);
+        float *to_part = sums.at + it.part * sums.next + (32 * kw + (lane & 31)) * a.dim;
 #pragma unroll
         for (int db = 0; db < DB; ++db)
 #pragma unroll
@@ -482,7 +519,7 @@ template <class T, int DP> __global__ __launch_bounds__(DP == 128 ? 512 : 256, 2
                 const int x = 32 * db + c_row(i, lane);
                 if (x >= a.dim) continue;
                 *(float4 *)(to_part + x) = make_float4(dk[db][i], dk[db][i + 1], dk[db][i + 2], dk[db][i + 3]);
-                *(float4 *)(to_part + (int64_t)128 * a.dim + x) = make_float4(dv[db][i], dv[db][i + 1], dv[db][i + 2], dv[db][i + 3]);
+                *(float4 *)(to_part + 128 * a.dim + x) = make_float4(dv[db][i], dv[db][i + 1], dv[db][i + 2], dv[db][i + 3]);
             }
         return;
     }
@@ -492,17 +529,21 @@ template <class T, int DP> __global__ __launch_bounds__(DP == 128 ? 512 : 256, 2
 
 // the parts of the key tiles that were cut, summed in their order: a block to 8 keys of a tile, 32 lanes to a key, 4 values each
 template <class T> __global__ __launch_bounds__(NT) void join_keys(AttendArgs a) {
-    const int group = blockIdx.x / (16 * a.split), at_tile = blockIdx.x / 16 % a.split, k0 = at_tile * 128;
-    const int b = group / a.kv_heads, hk = group % a.kv_heads, in = blockIdx.x % 16 * 8 + threadIdx.x / 32, x = threadIdx.x % 32 * 4;
+    const int in = blockIdx.x % 16 * 8 + threadIdx.x / 32, x = threadIdx.x % 32 * 4, hk = blockIdx.x / 16 % a.kv_heads, slot = blockIdx.x / (16 * a.kv_heads);
+    const bool all = a.usual > 1;      // else only tiles of sinks are cut, and the grid has no others
+    const int b = all ? slot_sequence(a, slot, a.k_offsets, a.total_k, 1) : slot / a.sink_tiles;
     const Sequence s = sequence_of(a, b);
-    if (k0 + in >= s.nk || x >= a.dim) return;
+    const int at_tile = all ? (int)(slot - tile_slot(a, b, s.k0, 1)) : slot % a.sink_tiles;
+    if (at_tile < 0 || at_tile >= a.tiles || (int64_t)at_tile * 128 + in >= s.nk || x >= a.dim) return;
+    const int k0 = at_tile * 128;
     const KeyTile t = key_tile(a, s, k0, min(k0 + 128, s.nk));
     const int parts = key_parts(a, at_tile, t.count);
     if (parts == 1) return;
-    const float *from = a.part_out + ((((int64_t)group * a.split + at_tile) * a.parts) * 256 + in) * a.dim + x;
+    const KeySums sums = key_sums(a, s, b, hk, at_tile);
+    const float *from = sums.at + in * a.dim + x;
     float4 k = make_float4(0.f, 0.f, 0.f, 0.f), v = k;
-    for (int p = 0; p < parts; ++p, from += (int64_t)256 * a.dim) {
-        const float4 y = *(const float4 *)from, z = *(const float4 *)(from + (int64_t)128 * a.dim);
+    for (int p = 0; p < parts; ++p, from += sums.next) {
+        const float4 y = *(const float4 *)from, z = *(const float4 *)(from + 128 * a.dim);
         k.x += y.x; k.y += y.y; k.z += y.z; k.w += y.w;
         v.x += z.x; v.y += z.y; v.z += z.z; v.w += z.w;
     }
@@ -510,6 +551,19 @@ template <class T> __global__ __launch_bounds__(NT) void join_keys(AttendArgs a)
     *(u32x2 *)(a.dk.p + 2 * (row * a.dk.row + (int64_t)hk * a.dk.head + x)) = (u32x2){T::pack(k.x, k.y), T::pack(k.z, k.w)};
     *(u32x2 *)(a.dv.p + 2 * (row * a.dv.row + (int64_t)hk * a.dv.head + x)) = (u32x2){T::pack(v.x, v.y), T::pack(v.z, v.w)};
 }
+
+// tiles of 128 `rows`, `tiles` in the longest sequence, and their numbers (tile_slot)
+void number(AttendArgs &a, int64_t tiles, int64_t rows) {
+    const int64_t close = rows / 128 + a.batch, wide = tiles * a.batch;
+    a.tiles = (int)tiles;
+    a.packed = close < wide;
+    a.slots = std::min(close, wide);
+}
+
+// floats of the sums of parts of row tiles, and of key tiles without sinks and with
+int64_t row_sums(const AttendArgs &a) { return a.parts > 1 ? a.slots * a.kv_heads * a.parts * 128 * a.dim : 0; }
+int64_t usual_sums(const AttendArgs &a) { return a.usual > 1 ? a.slots * a.kv_heads * a.usual * 256 * a.dim : 0; }
+int64_t sink_sums(const AttendArgs &a) { return a.sink_slots * a.sink_tiles * a.kv_heads * 256 * a.dim; }
 
 // How grad_keys is cut.  A block has a CU to itself at head sizes above 64, half of one below: 256 or 512 places.  Blocks go to the XCDs in
 // turn, whatever their length, so that a little more than one round of them takes as long as two.
@@ -519,6 +573,8 @@ template <class T> __global__ __launch_bounds__(NT) void join_keys(AttendArgs a)
 // Else lengths fall to nothing along the keys, and p parts of the longest tile make (p + 1) / 2 to a tile: as many as fill 88 % of one
 // round or, if that is fewer than three, two, whose second ones are what others lack.  All gradients of 6709 tokens, 4 heads, one key
 // head: 692 us whole, 397 in 2 parts, 249 in 4, 202 in 6, 232 in 8; of 4 x 2048, 16 heads, 4 key heads: 322, 286 in 2, 296 in 3, 326 in 4.
+// The sums of parts without sinks are those of at most four rounds of blocks, 134 MB.  Tiles of sinks have parts by the rows that see them: where
+// these would be more than eight rounds (268 MB), which takes hundreds of sinks or sequences, their parts get longer.
 void cut_keys(AttendArgs &a, int64_t max_k) {
     const int64_t tiles = cdiv(max_k, 128), all = all_tiles(a, tiles, a.total_k), places = a.dim > 64 ? 256 : 512, ends = a.dim > 64 ? 12 : 4;
     const int64_t longest = std::max<int64_t>(1, cdiv(a.max_q, RT) * a.group);
@@ -542,12 +598,25 @@ void cut_keys(AttendArgs &a, int64_t max_k) {
         parts = std::max<int64_t>(1, std::min(parts, usual / 2));
     }
     const int64_t chunk = cdiv(usual, parts);
-    a.tiles = (int)tiles;
+    number(a, tiles, a.total_k);
     a.chunk = (int)chunk;
     a.usual = (int)cdiv(usual, chunk);
-    a.split = (int)(a.usual > 1 ? tiles : sinks);
-    a.parts = (int)std::max<int64_t>(a.usual, a.split ? cdiv(longest, chunk) : 1);
-    if (a.parts == 1) a.split = 0;
+    a.sink_tiles = (int)sinks;
+    a.sink_chunk = (int)longest;
+    a.sink_slots = 0;
+    const int64_t room = 8 * places / std::max<int64_t>(1, sinks * a.kv_heads), rows = (a.total_q / RT + a.batch) * a.group;
+    for (const bool packed : {false, true}) {        // the least chunk with no more numbers than there is room for, and of two the fewer numbers
+        const int64_t each = packed ? room - a.batch : room / a.batch;
+        if (sinks == 0 || each < 1) continue;
+        const int64_t least = std::max(chunk, packed ? rows / (each + 1) + 1 : cdiv(longest, each));
+        const int64_t slots = packed ? rows / least + a.batch : a.batch * cdiv(longest, least);
+        if (least >= longest || least > a.sink_chunk || (least == a.sink_chunk && slots >= a.sink_slots)) continue;
+        a.sink_chunk = (int)least;
+        a.sink_packed = packed;
+        a.sink_slots = slots;
+    }
+    a.sink_parts = (int)cdiv(longest, a.sink_chunk);
+    a.parts = std::max(a.usual, a.sink_parts);
 }
 
 // How grad_rows is cut, at two blocks to a CU: parts of 10 key tiles or more fill the 512 places, where the row tiles do not; of tiles whose
@@ -555,7 +624,7 @@ void cut_keys(AttendArgs &a, int64_t max_k) {
 // 14 parts; four heads, 210: 158 whole, 90 + 9 in 3.  Shorter parts cost as much as they save (4 x 1024 tokens, 16 key tiles, 256 row
 // tiles: all gradients 49 us whole, 61 in two parts).
 void cut_rows(AttendArgs &a, int64_t max_k) {
-    a.tiles = (int)cdiv((int64_t)a.max_q * a.group, 128);
+    number(a, cdiv((int64_t)a.max_q * a.group, 128), a.total_q * a.group);
     const int64_t longest = std::max<int64_t>(1, cdiv(max_k, 64)), items = all_tiles(a, a.tiles, a.total_q * a.group);
     const int64_t most = a.window ? std::min(longest, cdiv((int64_t)a.window + cdiv(128, a.group), 64) + 1 + cdiv(a.sinks, 64)) : longest;
     const bool even = most < longest || !a.causal || 2 * (int64_t)a.max_q < max_k;
@@ -566,36 +635,39 @@ void cut_rows(AttendArgs &a, int64_t max_k) {
 
 // items of a group: the usual parts of all tiles, the other parts of the sinks' tiles (in rows of `tiles`, as block_of counts)
 int64_t key_items(const AttendArgs &a) {
-    const int64_t sinks = a.parts > a.usual ? std::min<int64_t>(a.tiles, cdiv(a.sinks, 128)) : 0;
-    return (int64_t)a.tiles * (a.usual + cdiv(sinks * (a.parts - a.usual), a.tiles));
+    return (int64_t)a.tiles * (a.usual + cdiv((int64_t)a.sink_tiles * (a.parts - a.usual), a.tiles));
 }
 
 int64_t stat_floats(const AttendArgs &a) { return cdiv(2 * a.total_q * a.heads, 64) * 64; }
 
 template <class T, int DP> void launch(AttendArgs a, int64_t max_k, hipStream_t st) {
     AttendArgs keys = a;                       // what cannot be launched is refused before anything is
-    int64_t key_blocks = 0;
+    int64_t key_blocks = 0, row_joins = 0, key_joins = 0;
     cut_rows(a, max_k);
     const int64_t row_blocks = attend_blocks(a, (int64_t)a.tiles * a.parts);
-    if (a.parts > 1 && (int64_t)a.groups * a.tiles * 16 >= 1 << 24) fail(F3M_ERR_UNSUPPORTED, "attention: too many sequences for one call's gradients");
+    if (a.parts > 1) row_joins = a.slots * a.kv_heads * 16;
     if (max_k && a.total_k) {
         cut_keys(keys, max_k);
         key_blocks = attend_blocks(keys, key_items(keys));
-        if ((int64_t)keys.groups * keys.split * 16 >= 1 << 24) fail(F3M_ERR_UNSUPPORTED, "attention: too many sequences for one call's gradients");
+        keys.sink_out = keys.part_out + usual_sums(keys);
+        // tiles of sinks are no more than a grid has room for, cut or not
+        const int64_t sink_joins = (int64_t)keys.groups * keys.sink_tiles * 16;
+        key_joins = keys.usual > 1 ? keys.slots * a.kv_heads * 16 : keys.sink_parts > 1 ? sink_joins : 0;
+        if (sink_joins >= 1 << 24) fail(F3M_ERR_UNSUPPORTED, "attention: too many sequences for one call's gradients");
     }
     if (a.max_q && a.total_q) {
         grad_rows<T, DP><<<dim3((uint32_t)row_blocks), NT, 0, st>>>(a);
         F3M_HIP(hipGetLastError());
-        if (a.parts > 1) {
-            join_rows<T><<<dim3((uint32_t)((int64_t)a.groups * a.tiles * 16)), NT, 0, st>>>(a);
+        if (row_joins) {
+            join_rows<T><<<dim3((uint32_t)row_joins), NT, 0, st>>>(a);
             F3M_HIP(hipGetLastError());
         }
     }
     if (key_blocks) {
         grad_keys<T, DP><<<dim3((uint32_t)key_blocks), DP == 128 ? 512 : 256, 0, st>>>(keys);
         F3M_HIP(hipGetLastError());
-        if (keys.split) {
-            join_keys<T><<<dim3((uint32_t)((int64_t)keys.groups * keys.split * 16)), NT, 0, st>>>(keys);
+        if (key_joins) {
+            join_keys<T><<<dim3((uint32_t)key_joins), NT, 0, st>>>(keys);
             F3M_HIP(hipGetLastError());
         }
     }
@@ -605,13 +677,13 @@ template <class T, int DP> void launch(AttendArgs a, int64_t max_k, hipStream_t 
 
 int64_t attend_grad_workspace(AttendArgs a, int64_t max_k) {
     int64_t floats = 0;                    // of the parts of either kernel, one after the other
-    if (a.max_q && a.total_q) {
+    if (a.groups && a.max_q && a.total_q) {
         cut_rows(a, max_k);
-        if (a.parts > 1) floats = (int64_t)a.groups * a.tiles * a.parts * 128 * a.dim;
+        floats = row_sums(a);
     }
-    if (max_k && a.total_k) {
+    if (a.groups && max_k && a.total_k) {
         cut_keys(a, max_k);
-        floats = std::max(floats, (int64_t)a.groups * a.split * (a.split ? a.parts : 0) * 256 * a.dim);
+        floats = std::max(floats, usual_sums(a) + sink_sums(a));
     }
     return (stat_floats(a) + floats) * (int64_t)sizeof(float);
 }

@@ -121,3 +121,64 @@ def test_a_first_offset_below_zero_is_cut_to_zero(nq, nk, group, first):
     f3m.attention(q.to(DEV), k.to(DEV), v.to(DEV), dev_offsets([first, nq]), dev_offsets([first, nk]), scale=0.125, out=out, lse=lse)
     au.close(out, want, "out")
     au.close(lse, want, "lse")
+
+
+@pytest.mark.parametrize("type,D", [(BF, 64), (HF, 128), (BF, 40)])
+@pytest.mark.parametrize("lengths,Hq,Hk,keys,how", [
+    ([1900, 5, 0, 70, 300, 1], 1, 1, None, {}), ([5, 1, 1600, 64, 129], 2, 1, None, dict(causal=False)),     # packed numbers, rows and keys in parts
+    ([1500, 1500], 2, 2, None, {}),                                                                          # all alike
+    ([1400, 3, 700, 64], 2, 1, None, dict(window=100, sinks=3)), ([1300], 4, 2, None, dict(window=60, sinks=300)),
+    ([2048] + [100, 3, 260, 0, 64] * 3, 16, 8, None, dict(window=64, sinks=5000)),            # longer parts for tiles of sinks: so many are there
+    ([260] * 40, 32, 32, None, dict(window=1, sinks=300)),                                   # none
+    ([900, 10, 900], 3, 1, None, dict(window=200)), ([40, 0, 700], 4, 2, [2000, 300, 900], dict(window=500, sinks=140))])
+def test_parts_of_uneven_batches_stay_in_their_workspace(type, D, lengths, Hq, Hk, keys, how):
+    """the gradients through the C entry, with no byte of workspace more than asked for and a pattern behind it"""
+    pad = 30              # rows before the first sequence and behind the last
+    nk = keys or lengths
+    qo, ko = ([pad + x for x in au.offsets(n)] for n in (lengths, nk))
+    q, do = (normal((qo[-1] + pad, Hq, D), 90 + i, type) for i in (0, 1))
+    k, v = (normal((ko[-1] + pad, Hk, D), 92 + i, type) for i in (0, 1))
+    want = au.batch(q, k, v, qo, ko, 0.125, dout=do, **how)
+    print("uneven", type, D, lengths, Hq, Hk, keys, how, flush=True)
+    dev = {n: x.to(DEV) for n, x in dict(q=q, k=k, v=v, dout=do).items()}
+    offs = [dev_offsets(qo), dev_offsets(ko)]
+    out, lse = f3m.attention(dev["q"], dev["k"], dev["v"], *offs, max_q=max(lengths), max_k=max(nk), scale=0.125, **how)
+    a = f3m.AttentionArgs(dtype=0 if type == BF else 1, batch=len(lengths), heads=Hq, kv_heads=Hk, head_dim=D, causal=int(how.get("causal", True)),
+                          window=how.get("window", 0), sinks=how.get("sinks", 0), scale=0.125, max_q=max(lengths), max_k=max(nk), total_q=q.shape[0],
+                          total_k=k.shape[0], q_offsets=offs[0].data_ptr(), k_offsets=offs[1].data_ptr())
+    rows = {n: f3m.Rows(x.data_ptr(), x.shape[1] * D, D) for n, x in dict(dev, out=out).items()}
+    a.q, a.k, a.v = rows["q"], rows["k"], rows["v"]
+    need = f3m.lib().f3m_attention_grad_workspace(ctypes.byref(a))
+    w = torch.full((need + (1 << 20),), 0xa5, dtype=torch.uint8, device=DEV)
+    got = {n: torch.full_like(dev[n[1]], 7.0) for n in ("dq", "dk", "dv")}
+    to = [f3m.Rows(x.data_ptr(), x.shape[1] * D, D) for x in got.values()]
+    assert f3m.lib().f3m_attention_grad(ctypes.byref(a), ctypes.byref(rows["dout"]), ctypes.byref(rows["out"]), lse.data_ptr(), *(ctypes.byref(x) for x in to),
+                                        w.data_ptr(), need, torch.cuda.current_stream().cuda_stream) == 0
+    assert (w[need:] == 0xa5).all()
+    for name, x in got.items():
+        au.close(x, want, name)
+        assert (x[:pad] == 7).all() and (x[-pad:] == 7).all()
+
+
+@pytest.mark.parametrize("window,sinks", [(0, 0), (100, 300)])
+def test_offsets_that_lie_stay_in_the_workspace(window, sinks):
+    """falling offsets and such past the tensors, in a call whose gradients go in parts: no byte past the workspace or in rows of no sequence"""
+    n, D = 2000, 64
+    q, k, v, do = (normal((n, 1, D), 95 + i, BF).to(DEV) for i in range(4))
+    off = dev_offsets([10, 1600, 40, 1990, -5, 10 ** 9, 1700])
+    a = f3m.AttentionArgs(dtype=0, batch=6, heads=1, kv_heads=1, head_dim=D, causal=1, window=window, sinks=sinks, scale=0.125, max_q=1990, max_k=1990,
+                          total_q=n, total_k=n, q_offsets=off.data_ptr(), k_offsets=off.data_ptr())
+    out, lse = torch.zeros_like(q), torch.zeros((n, 1), device=DEV)
+    rows = [f3m.Rows(x.data_ptr(), D, D) for x in (q, k, v, do, out)]
+    a.q, a.k, a.v = rows[:3]
+    grads = [torch.full_like(q, 7.0) for _ in range(3)]
+    to = [ctypes.byref(f3m.Rows(x.data_ptr(), D, D)) for x in grads]
+    need = f3m.lib().f3m_attention_grad_workspace(ctypes.byref(a))
+    w = torch.full((need + (1 << 20),), 0xa5, dtype=torch.uint8, device=DEV)
+    assert f3m.lib().f3m_attention_grad(ctypes.byref(a), ctypes.byref(rows[3]), ctypes.byref(rows[4]), lse.data_ptr(), *to, w.data_ptr(), need,
+                                        torch.cuda.current_stream().cuda_stream) == 0
+    assert (w[need:] == 0xa5).all()
+    need = f3m.lib().f3m_attention_workspace(ctypes.byref(a))
+    w = torch.full((need + (1 << 20),), 0xa5, dtype=torch.uint8, device=DEV)
+    assert f3m.lib().f3m_attention(ctypes.byref(a), ctypes.byref(rows[4]), lse.data_ptr(), w.data_ptr(), need, torch.cuda.current_stream().cuda_stream) == 0
+    assert (w[need:] == 0xa5).all()
