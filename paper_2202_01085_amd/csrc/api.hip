@@ -157,6 +157,7 @@ f3m::AttendArgs attend_args(const f3m_attention_args &p) {
     a.total_q = p.total_q;
     a.total_k = p.total_k;
     a.max_q = (int)std::min<int64_t>(p.max_q, p.total_q);
+    a.max_k = p.max_k;
     a.q_offsets = p.q_offsets;
     a.k_offsets = p.k_offsets;
     a.q = rows_of(p.q, p.total_q, p.head_dim);

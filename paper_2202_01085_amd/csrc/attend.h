@@ -24,7 +24,7 @@ struct AttendArgs {
     int causal, window, sinks;
     float scale;
     int64_t total_q, total_k;
-    int max_q;
+    int max_q, max_k;
     const int *q_offsets, *k_offsets;         // null: one sequence
     Rows q, k, v, out;
     float *lse;                               // (rows of q, heads)

@@ -317,23 +317,24 @@ template <class T, int DP> __global__ __launch_bounds__(DP == 128 ? 512 : 256, 2
         if (at_tile >= a.sink_tiles) return;
     }
     const int k0 = at_tile * 128;
-    if (k0 >= s.nk) return;
+    const int nk = min(s.nk, a.max_k);                               // keys whose gradients are asked for
+    if (k0 >= nk) return;
     const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6), kw = wave & 3, half = wave >> 2;
     const int off = s.nk - s.nq;                                     // position of token 0
-    const KeyTile t = key_tile(a, s, k0, min(k0 + 128, s.nk));
+    const KeyTile t = key_tile(a, s, k0, min(k0 + 128, nk));
     const int parts = key_parts(a, at_tile, t.count);
     if (it.part >= parts) return;
     const int chunk = key_chunk(a, at_tile), begin = it.part * chunk, end = it.part + 1 < parts ? begin + chunk : t.count;
 
-    const int w0 = k0 + 32 * kw, key = w0 + (lane & 31), kept = min(key, s.nk - 1);
-    const bool valid = key < s.nk, idle = w0 >= s.nk;
+    const int w0 = k0 + 32 * kw, key = w0 + (lane & 31), kept = min(key, nk - 1);
+    const bool valid = key < nk, idle = w0 >= nk;
     // tokens [from, to) see this lane's key
     const int from = !valid ? t.hi : a.causal ? max(key - off, 0) : 0;
     const int to = a.causal && a.window && key >= a.sinks ? (int)min((int64_t)t.hi, (int64_t)key + a.window - off) : t.hi;
-    const KeyTile mine = key_tile(a, s, w0, min(w0 + 32, s.nk));     // of the wave: it has nothing to do elsewhere
+    const KeyTile mine = key_tile(a, s, w0, min(w0 + 32, nk));     // of the wave: it has nothing to do elsewhere
     // tokens [all.x, all.y) see all keys x .. y - 1
     auto seen_by_all = [&](int x, int y) {
-        if (y > s.nk) return make_int2(0, 0);
+        if (y > nk) return make_int2(0, 0);
         if (!a.causal) return make_int2(0, t.hi);
         return make_int2(y - 1 - off, a.window && y > a.sinks ? (int)min((int64_t)t.hi, (int64_t)x + a.window - off) : t.hi);
     };
@@ -350,7 +351,7 @@ template <class T, int DP> __global__ __launch_bounds__(DP == 128 ? 512 : 256, 2
     if (V_LDS)
         for (int at = tid; at < 128 * (DP / 8); at += THREADS) {
             const int r = at / (DP / 8), piece = at % (DP / 8);
-            *(u32x4 *)(vt + tile_at<DP>(r, piece)) = load_piece<DP>(a.v.p, (int64_t)(s.k0 + min(k0 + r, s.nk - 1)) * a.v.row + (int64_t)hk * a.v.head, piece, a.dim);
+            *(u32x4 *)(vt + tile_at<DP>(r, piece)) = load_piece<DP>(a.v.p, (int64_t)(s.k0 + min(k0 + r, nk - 1)) * a.v.row + (int64_t)hk * a.v.head, piece, a.dim);
         }
 #pragma unroll
     for (int db = 0; db < DB; ++db) { dk[db] = (f32x16)0.f; dv[db] = (f32x16)0.f; }
@@ -534,9 +535,10 @@ template <class T> __global__ __launch_bounds__(NT) void join_keys(AttendArgs a)
     const int b = all ? slot_sequence(a, slot, a.k_offsets, a.total_k, 1) : slot / a.sink_tiles;
     const Sequence s = sequence_of(a, b);
     const int at_tile = all ? (int)(slot - tile_slot(a, b, s.k0, 1)) : slot % a.sink_tiles;
-    if (at_tile < 0 || at_tile >= a.tiles || (int64_t)at_tile * 128 + in >= s.nk || x >= a.dim) return;
+    const int nk = min(s.nk, a.max_k);
+    if (at_tile < 0 || (int64_t)at_tile * 128 + in >= nk || x >= a.dim) return;
     const int k0 = at_tile * 128;
-    const KeyTile t = key_tile(a, s, k0, min(k0 + 128, s.nk));
+    const KeyTile t = key_tile(a, s, k0, min(k0 + 128, nk));
     const int parts = key_parts(a, at_tile, t.count);
     if (parts == 1) return;
     const KeySums sums = key_sums(a, s, b, hk, at_tile);

@@ -182,3 +182,18 @@ def test_offsets_that_lie_stay_in_the_workspace(window, sinks):
     w = torch.full((need + (1 << 20),), 0xa5, dtype=torch.uint8, device=DEV)
     assert f3m.lib().f3m_attention(ctypes.byref(a), ctypes.byref(rows[4]), lse.data_ptr(), w.data_ptr(), need, torch.cuda.current_stream().cuda_stream) == 0
     assert (w[need:] == 0xa5).all()
+
+
+@pytest.mark.parametrize("n,most", [(300, 130), (300, 1), (1500, 1000), (1500, 0)])
+@pytest.mark.parametrize("how", [{}, dict(window=50, sinks=200)])
+def test_gradients_of_keys_from_max_k_on_are_left_alone(n, most, how):
+    """also of those that share a tile with keys before it, whole or in parts"""
+    q, k, v, do = (normal((n, 1, 64), 60 + i, BF).to(DEV) for i in range(4))
+    off = dev_offsets([0, n])
+    want = au.batch(q.cpu(), k.cpu(), v.cpu(), [0, n], [0, n], 0.125, dout=do.cpu(), **how)
+    out, lse = f3m.attention(q, k, v, scale=0.125, **how)
+    grads = [torch.full_like(q, 7.0) for _ in range(3)]
+    f3m.attention_grad(do, q, k, v, out, lse, off, off, n, most, scale=0.125, dq=grads[0], dk=grads[1], dv=grads[2], **how)
+    for x, name in zip(grads[1:], ("dk", "dv")):
+        au.close(x[:most], {y: want[y][:most] for y in (name, name + "_tol")}, name)
+        assert (x[most:] == 7).all()
