@@ -525,7 +525,8 @@ class KVCache:
 
     k, v (pages, kv_heads, page_size, head_dim), contiguous, of bfloat16, float16 or float8_e4m3fn; for the last k_exp and v_exp
     (pages, kv_heads, page_size) uint8, the rows' exponents: a value is code * 2^(byte - 127).  Slot s is row s % page_size of
-    page s // page_size.  KVCache.empty makes the tensors."""
+    page s // page_size.  KVCache.empty makes the tensors.  A cache keeps to its tensors and to where they lie: a larger one is a new
+    KVCache of new tensors."""
 
     def __init__(self, k, v, k_exp=None, v_exp=None):
         if not (isinstance(k, torch.Tensor) and k.is_cuda and k.dim() == 4 and k.dtype in DTYPES):
@@ -538,9 +539,20 @@ class KVCache:
             at_k_exp, at_v_exp = _device_array(k_exp, "k_exp", torch.uint8, device, rows), _device_array(v_exp, "v_exp", torch.uint8, device, rows)
         elif k_exp is not None or v_exp is not None:
             raise ValueError("k_exp and v_exp belong to 8-bit caches")
-        self.k, self.v, self.k_exp, self.v_exp = k, v, k_exp, v_exp
+        self._tensors = k, v, k_exp, v_exp
         pages, heads, page_size, dim = shape
-        self._c = CacheInfo(DTYPES[dtype], heads, dim, page_size, pages, at_k, at_v, at_k_exp, at_v_exp)
+        self._at = at_k, at_v, at_k_exp, at_v_exp
+        self._c = CacheInfo(DTYPES[dtype], heads, dim, page_size, pages, *self._at)
+
+    # without setters: calls go by the addresses of these tensors
+    k, v, k_exp, v_exp = (property(lambda self, i=i: self._tensors[i]) for i in range(4))
+
+    def _info(self):
+        """what the library gets; tensors that were resized or given other memory are refused, as their old one may be gone"""
+        for t, at in zip(self._tensors, self._at):
+            if t is not None and t.data_ptr() != (at or 0):
+                raise ValueError("the cache's tensors no longer lie where they did: make a new KVCache of them")
+        return self._c
 
     @classmethod
     def empty(cls, pages, page_size, kv_heads, head_dim, dtype=torch.float8_e4m3fn, device="cuda"):
@@ -552,7 +564,7 @@ class KVCache:
         return cls(zeros(shape, dtype), zeros(shape, dtype), *exp)
 
     def _move(self, call, k, v, slots, handle):
-        device, c = self.k.device, self._c
+        device, c = self.k.device, self._info()
         rk = _rows(k, "k")
         shape = k.shape
         if shape[1:] != (c.kv_heads, c.head_dim) or k.device != device:
@@ -586,7 +598,7 @@ class KVCache:
         Key j of sequence b lies in page table[b, j // page_size] (int32, on the device), j < lengths[b] (int32, on the device).
         q_offsets as for attention(); without, every sequence has the same number of new tokens (rows of q / sequences).
         max_k: the longest length (default: what the table has room for)."""
-        device, c = self.k.device, self._c
+        device, c = self.k.device, self._info()
         if not (isinstance(table, torch.Tensor) and table.is_cuda and table.dtype == torch.int32 and table.dim() == 2 and table.device == device):
             raise TypeError("table must be an int32 tensor (sequences, pages) on the cache's device")
         batch, cols = table.shape
