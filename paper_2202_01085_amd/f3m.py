@@ -6,6 +6,7 @@ library is missing, importing a symbol from it raises.
 """
 import ctypes
 import os
+import warnings
 
 import numpy as np
 import torch
@@ -431,6 +432,16 @@ def _device_array(t, name, dtype, device, shape):
     return t.data_ptr() or None
 
 
+def _no_graph(name, *tensors):
+    """results of this library carry no graph of torch's: who would expect one is told"""
+    if torch.is_grad_enabled():
+        for t in tensors:
+            if t.requires_grad:
+                warnings.warn("%s: the results carry no graph, although an argument requires gradients: those come from attention_grad(); "
+                              "torch.no_grad() around the call says that this is meant" % name, stacklevel=3)
+                return
+
+
 def _attention_args(q, shape, rq, rk, rv, kv_heads, total_k, q_offsets, k_offsets, max_q, max_k, scale, causal, window, sinks):
     rows, heads, dim = shape
     batch, qo = 1, None
@@ -482,8 +493,11 @@ def attention(q, k, v, q_offsets=None, k_offsets=None, max_q=None, max_k=None, s
     q_offsets[b + 1] - 1 and the same of k_offsets (int32, on the device; without: one sequence).  max_q and max_k are the longest
     sequence's (default: all rows; smaller ones make for fewer work items).  causal: token i of nq sees the keys up to
     nk - nq + i; window > 0: the last `window` of those and the first `sinks`.  scale: 1/sqrt(head_dim) by default.
-    lse (rows, heads) float32: logarithms of the sums, -inf where nothing is visible (and out is 0)."""
+    lse (rows, heads) float32: logarithms of the sums, -inf where nothing is visible (and out is 0).  Rows of no sequence, and tokens from
+    max_q on, keep what out and lse held; without out and lse that is whatever their memory held.
+    The results carry no graph of torch's (a warning says so where q, k or v require gradients): attention_grad() gives the gradients."""
     a = _packed_args(q, k, v, q_offsets, k_offsets, max_q, max_k, scale, causal, window, sinks)
+    _no_graph("attention", q, k, v)
     device, shape = q.device, q.shape
 
     def call(handle):
@@ -500,7 +514,8 @@ def attention(q, k, v, q_offsets=None, k_offsets=None, max_q=None, max_k=None, s
 
 def attention_grad(dout, q, k, v, out, lse, q_offsets=None, k_offsets=None, max_q=None, max_k=None, scale=None, causal=True, window=0,
                    sinks=0, dq=None, dk=None, dv=None, stream=None):
-    """f3m_attention_grad: (dq, dk, dv) from the gradient dout of out, with the out and lse of attention() and its arguments."""
+    """f3m_attention_grad: (dq, dk, dv) from the gradient dout of out, with the out and lse of attention() and its arguments.  Gradients of rows
+    of no sequence, of tokens from max_q and of keys from max_k on keep what dq, dk and dv held (without those, whatever their memory held)."""
     a = _packed_args(q, k, v, q_offsets, k_offsets, max_q, max_k, scale, causal, window, sinks)
     device, dtype, shape = q.device, q.dtype, q.shape
     g, o = _rows(dout, "dout", dtype, device, shape), _rows(out, "out", dtype, device, shape)
@@ -597,7 +612,7 @@ class KVCache:
 
         Key j of sequence b lies in page table[b, j // page_size] (int32, on the device), j < lengths[b] (int32, on the device).
         q_offsets as for attention(); without, every sequence has the same number of new tokens (rows of q / sequences).
-        max_k: the longest length (default: what the table has room for)."""
+        max_k: the longest length (default: what the table has room for).  There are no gradients over a cache."""
         device, c = self.k.device, self._info()
         if not (isinstance(table, torch.Tensor) and table.is_cuda and table.dtype == torch.int32 and table.dim() == 2 and table.device == device):
             raise TypeError("table must be an int32 tensor (sequences, pages) on the cache's device")
@@ -609,6 +624,7 @@ class KVCache:
         shape = q.shape
         if q.device != device:
             raise ValueError("q must be on the cache's device")
+        _no_graph("KVCache.attention", q)
         ln = _device_array(lengths, "lengths", torch.int32, device, (batch,))
 
         def call(handle):
