@@ -299,7 +299,7 @@ f3m_status f3m_cg_solve(f3m_plan_t *plan, float lambda, const float *b, float *x
  * least the same elements of o NaN or infinite, one in k, q or dout all that depends on the pair.
  * Offsets and lengths are read on the device and not checked by the host: such as lie outside the tensors are cut to
  * what exists, and no access leaves the tensors.  Offsets do not fall; if they do, results are not defined.
- * A row whose visible scores are all -inf counts as one that sees no key.
+ * A row whose visible scores are all -inf counts as one that sees no key.  Scores may have any size that fp32 holds.
  * Limits: head_dim a multiple of 8 up to 128; data 16-byte aligned, strides multiples of 8 values, those between rows
  * below 2^22; fewer than 2^31 - 65536 rows.
  * Every call is asynchronous on `stream` and allocates nothing; the caller brings the workspace (the *_workspace calls
@@ -344,7 +344,9 @@ f3m_status f3m_attention(const f3m_attention_args *args, const f3m_rows *out, fl
  * f3m_attention_grad - the gradients of a loss whose gradient with respect to o is dout: dq, dk, dv (overwritten, summed
  * over the heads that share a key head), from the out and lse of f3m_attention with the same arguments.  lse carries no
  * gradient.  The weights and their gradients are rounded to dtype for the products; in fp16 after scaling by powers of
- * two, so that small gradients keep their bits.
+ * two, so that small gradients keep their bits.  The weights are made again from lse, whose rounding to fp32 makes them off by
+ * 2^-24 |lse| of their size: not seen beside 2^-8 or 2^-11 up to a thousand, as much as those from 2^13 (fp16) or 2^16 (bf16) on; past
+ * 2^20 they are not to be used.
  */
 f3m_status f3m_attention_grad(const f3m_attention_args *args, const f3m_rows *dout, const f3m_rows *out, const float *lse,
                               const f3m_rows *dq, const f3m_rows *dk, const f3m_rows *dv, void *workspace,

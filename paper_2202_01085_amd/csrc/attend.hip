@@ -110,8 +110,11 @@ template <class T, int DP> struct Rows32 {
     // NB blocks of 32 keys from key0 on: read_k(base, ks) is the A operand of k from row `base` on, v lies in LDS at vt, all of it or (half
     // given) 16 rows at a time, which half(h) puts there.  edge: the mask cuts the tile for some row, or `good` (rows in pages of the cache) says
     // something.  Returns the bits of the keys that the row sees.
+    // An exponent is s c - m c + LIFT in one operation, whose second product is rounded, by up to 2^-25 of it, the same for all weights of a row.
+    // From 2^20 on that is not small any more, and from 2^31 on it would leave the range of exp2: with FAR m is taken off first in
+    // such rows; the others' results are the same bits either way.
     struct Whole {};
-    template <int NB, class ReadK, class Half = Whole>
+    template <int NB, bool FAR, class ReadK, class Half = Whole>
     __device__ __forceinline__ uint64_t step(const LaneReads<DP> &at, ReadK &&read_k, uint32_t vt, int key0, bool edge, uint64_t good, const Limits &mine, int sinks,
                                              float c, int lane, Half &&half = Whole{}) {
         constexpr bool HALVES = !std::is_same<typename std::decay<Half>::type, Whole>::value;
@@ -146,12 +149,13 @@ template <class T, int DP> struct Rows32 {
 #pragma unroll
                 for (int i = 0; i < 16; ++i) o[db][i] *= by;
         }
-        const float base = m == NO_KEY ? 0.f : LIFT - m * c;
+        const bool far = FAR && m != NO_KEY && !near(c);
+        const float off = far ? m : 0.f, base = m == NO_KEY ? 0.f : far ? LIFT : LIFT - m * c;
         float sums[2];
         auto weigh = [&](int kb, int from, int to) {
 #pragma unroll
             for (int i = from; i < to; ++i) {
-                s[kb][i] = __builtin_amdgcn_exp2f(__builtin_fmaf(s[kb][i], c, base));
+                s[kb][i] = __builtin_amdgcn_exp2f(__builtin_fmaf(FAR ? s[kb][i] - off : s[kb][i], c, base));
                 sums[i % 2] = i < 2 ? s[kb][i] : sums[i % 2] + s[kb][i];
             }
             if (to == 16) l += sums[0] + sums[1];
@@ -177,6 +181,7 @@ template <class T, int DP> struct Rows32 {
         }
         return seen;
     }
+    __device__ bool near(float c) const { return m == NO_KEY || fabsf(m * c) <= 0x1p20f; }
     __device__ bool finite() const {
         bool all = true;
 #pragma unroll
@@ -259,8 +264,9 @@ template <class T, int DP, bool E8> __global__ __launch_bounds__(NT, DP == 128 ?
     Row r;
     const int begin = n;
     // Tiles that the mask cuts are not cleaned of infinities and NaN in v at first: if none shows in the results, there was none that
-    // mattered.  Else all is done again with care.
-    auto pass = [&](bool careful) {
+    // mattered.  Else all is done again with care, and so it is where scores are too large for the shorter exponents.
+    auto pass = [&](auto with_care) {
+        constexpr bool careful = decltype(with_care)::value;
         n = begin;
         r.start(a, a.q.p, (int64_t)(s.q0 + token) * a.q.row + (int64_t)head * a.q.head, lane);
         auto step = [&](int buf, int key0, uint64_t ok, uint64_t odd) {
@@ -268,7 +274,7 @@ template <class T, int DP, bool E8> __global__ __launch_bounds__(NT, DP == 128 ?
             const bool full = key0 + KT <= wfirst.hi && (key0 >= wlast.lo || key0 + KT <= a.sinks) && ok == ~0ull && odd == 0;
             const uint32_t kt = lds_address(tile[buf][0]);
             if (none) return;
-            const uint64_t seen = r.template step<2>(at, [&](int base, int ks) { return at.row(kt, base, ks); }, lds_address(tile[buf][1]), key0, !full, ok, mine, a.sinks, c, lane);
+            const uint64_t seen = r.template step<2, careful>(at, [&](int base, int ks) { return at.row(kt, base, ks); }, lds_address(tile[buf][1]), key0, !full, ok, mine, a.sinks, c, lane);
             if (seen & odd) r.spoil = __builtin_nanf("");
         };
         if (n >= end) return;
@@ -329,8 +335,8 @@ template <class T, int DP, bool E8> __global__ __launch_bounds__(NT, DP == 128 ?
             }
         }
     };
-    pass(false);
-    if (__syncthreads_or(!r.finite())) pass(true);
+    pass(std::false_type{});
+    if (__syncthreads_or(!r.near(c) || !r.finite())) pass(std::true_type{});
     const float all = both_halves_sum(r.l), by = both_halves_sum(r.spoil) + (all > 0.f ? 1.f / all : all == all ? 0.f : all);
     const int64_t at_row = (int64_t)(s.q0 + token) * a.heads + head;
     if (a.parts > 1) {
@@ -470,7 +476,7 @@ template <class T, int DP, bool E8> __global__ __launch_bounds__(NT, E8 ? 2 : 1)
                     }
                     __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");
                 };
-                seen = r.template step<1>(at, read_k, kt, key0, !whole, good, mine, a.sinks, c, lane, half);
+                seen = r.template step<1, true>(at, read_k, kt, key0, !whole, good, mine, a.sinks, c, lane, half);
             } else {
                 if (!whole) {
 #pragma unroll 2
@@ -484,7 +490,7 @@ template <class T, int DP, bool E8> __global__ __launch_bounds__(NT, E8 ? 2 : 1)
                     }
                 }
                 __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");
-                seen = r.template step<1>(at, [&](int base, int ks) { return at.row(kt, base, ks); }, vt, key0, !whole, good, mine, a.sinks, c, lane);
+                seen = r.template step<1, true>(at, [&](int base, int ks) { return at.row(kt, base, ks); }, vt, key0, !whole, good, mine, a.sinks, c, lane);
             }
             if (!whole && __any(odd != 0)) {
 #pragma unroll 1

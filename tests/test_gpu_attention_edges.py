@@ -197,3 +197,22 @@ def test_gradients_of_keys_from_max_k_on_are_left_alone(n, most, how):
     for x, name in zip(grads[1:], ("dk", "dv")):
         au.close(x[:most], {y: want[y][:most] for y in (name, name + "_tol")}, name)
         assert (x[most:] == 7).all()
+
+
+@pytest.mark.parametrize("type,size", [(BF, 30.0), (HF, 150.0), (BF, 3e3), (HF, 1.3e4), (BF, 1e8), (BF, 1e15)])
+@pytest.mark.parametrize("D,nq,nk", [(64, 300, 300), (128, 200, 900), (64, 1, 3000), (128, 20, 700), (32, 70, 9000)])
+def test_scores_of_any_size_that_fp32_holds(type, size, D, nq, nk):
+    """scores up to 1e32: the weights are those of the differences to the largest one (mostly one key's alone)"""
+    q, k, v = normal((nq, 2, D), 1, type, size), normal((nk, 1, D), 2, type, size), normal((nk, 1, D), 3, type)
+    want = au.batch(q, k, v, [0, nq], [0, nk], 0.125)
+    print("large scores", type, size, D, nq, nk, float(want["lse"].abs().max()), flush=True)
+    out, lse = f3m.attention(q.to(DEV), k.to(DEV), v.to(DEV), scale=0.125)
+    au.close(lse, want, "lse")
+    # a score is off by up to FP32 of the sum of its products' sizes: rows where a second key comes within ten times that of the first are left out
+    s = torch.stack([q[:, h].double() @ k[:, 0].double().T for h in range(2)], 1) * 0.125
+    s = torch.where(au.visible(nq, nk, True, 0, 0)[:, None], s, torch.full((), -torch.inf, dtype=torch.float64))
+    top = s.topk(2, -1).values
+    mass = 0.125 * (torch.stack([q[:, h].double().abs() @ k[:, 0].double().abs().T for h in range(2)], 1)).amax(-1)
+    clear = ((top[..., 0] - top[..., 1]) > 10 * au.FP32 * mass) | (mass * au.FP32 < 2.0 ** -9)
+    assert clear.float().mean() > 0.9
+    au.close(out.cpu()[clear], {n: want[n][clear] for n in ("out", "out_tol")}, "out")
