@@ -296,7 +296,8 @@ f3m_status f3m_cg_solve(f3m_plan_t *plan, float lambda, const float *b, float *x
  * of those the last `window` (j > p - window) and the first `sinks` keys of the sequence.  A token that sees no key
  * (p < 0) gets o = 0 and lse = -inf, and adds nothing to the gradients.  What hidden keys hold (NaN, infinities)
  * reaches no token, nor do hidden tokens' values reach a key's gradients.  A NaN or infinity in a visible row of v makes at
- * least the same elements of o NaN or infinite, one in k, q or dout all that depends on the pair.
+ * least the same elements of o NaN or infinite (in some rows all of their elements NaN), one in k, q or dout all that depends on
+ * the pair; but a score of -inf counts as a weight of 0 or as NaN.
  * Offsets and lengths are read on the device and not checked by the host: such as lie outside the tensors are cut to
  * what exists, and no access leaves the tensors.  Offsets do not fall; if they do, results are not defined.
  * A row whose visible scores are all -inf counts as one that sees no key.  Scores may have any size that fp32 holds.
@@ -359,7 +360,8 @@ f3m_status f3m_attention_grad(const f3m_attention_args *args, const f3m_rows *do
  *   k_exp, v_exp  pages x kv_heads x page_size bytes, with F3M_E4M3 only (else NULL)
  * Slot s is row s % page_size of page s / page_size.  held = F3M_E4M3: a row's values are code * 2^(byte - 127); the byte is the
  * least that keeps the row's largest finite value within 448, from 1 to 254, so that writing rounds once, to e4m3, and
- * reading is exact (in fp16, values beyond its range become infinite).  Infinities and NaN are kept as NaN.  head_dim is a
+ * reading is exact (values that the range of the type read does not hold are rounded to it: to infinity, to a multiple of its
+ * smallest number).  Infinities and NaN are kept as NaN.  head_dim is a
  * multiple of 16 then.  page_size is a power of two from 8 to 1024.
  */
 typedef struct {

@@ -216,3 +216,61 @@ def test_scores_of_any_size_that_fp32_holds(type, size, D, nq, nk):
     clear = ((top[..., 0] - top[..., 1]) > 10 * au.FP32 * mass) | (mass * au.FP32 < 2.0 ** -9)
     assert clear.float().mean() > 0.9
     au.close(out.cpu()[clear], {n: want[n][clear] for n in ("out", "out_tol")}, "out")
+
+
+@pytest.mark.parametrize("type", [BF, HF])
+def test_every_code_with_every_exponent(type):
+    """what a cache holds, read as either type: the value, rounded to the type where its range does not hold it"""
+    codes, page = torch.arange(256, dtype=torch.uint8), 8
+    c = f3m.KVCache.empty(256, page, 1, 128, device=DEV)      # page b: exponent byte b, all codes in its first two rows
+    c.k.view(torch.uint8)[:, 0, :2] = codes.view(2, 128).to(DEV)
+    c.v.view(torch.uint8)[:, 0, :2] = codes.view(2, 128).to(DEV)
+    for x in (c.k_exp, c.v_exp):
+        x.copy_(torch.arange(256, dtype=torch.uint8, device=DEV)[:, None, None].expand(256, 1, page))
+    slots = (torch.arange(256)[:, None] * page + torch.arange(2)).flatten().to(DEV)
+    want = (codes.view(E8).double() * torch.exp2(torch.arange(256).double() - 127)[:, None]).to(type)[1:255]
+    for x in c.read(slots, dtype=type):
+        x = x.cpu().view(256, 256)[1:255]
+        assert torch.equal(torch.isnan(x), torch.isnan(want))
+        assert torch.equal(torch.nan_to_num(x, nan=0.0, posinf=1e9, neginf=-1e9), torch.nan_to_num(want, nan=0.0, posinf=1e9, neginf=-1e9))
+
+
+@pytest.mark.parametrize("type,held,D", [(BF, BF, 8), (HF, HF, 24), (BF, BF, 40), (HF, HF, 72), (BF, BF, 104), (BF, E8, 16), (HF, E8, 48), (BF, E8, 112)])
+@pytest.mark.parametrize("causal", [True, False])
+@pytest.mark.parametrize("news", [[1, 1, 1, 0], [60, 1, 17, 5]])
+def test_caches_of_odd_heads_strided_tensors_and_large_pages(type, held, D, causal, news):
+    """head sizes inside a tile, pages of 512 and 1024, the table a part of a wider one, q and out views of wider tensors with heads first"""
+    lengths, page = [1100, 3, 513, 40], 512 if D % 16 else 1024
+    c, table, k, v = paged(type, held, lengths, 2, D, page, D)
+    wide = torch.full((4, 9), -5, dtype=torch.int32, device=DEV)
+    wide[:, 2:2 + table.shape[1]] = table.to(DEV)
+    qo, ko, Hq = au.offsets(news), au.offsets(lengths), 6
+    n = qo[-1]
+    q = normal((n, Hq, D), 5, type)
+    room = torch.full((Hq, n, D + 16), NAN, dtype=type, device=DEV)
+    room[:, :, :D] = q.transpose(0, 1).to(DEV)
+    res = torch.full((Hq, n + 2, D + 8), 7.0, dtype=type, device=DEV)
+    want = au.batch(q, k, v, qo, ko, 0.125, causal)
+    print("odd caches", type, held, D, causal, news, flush=True)
+    out, lse = c.attention(room[:, :, :D].transpose(0, 1), wide[:, 2:2 + table.shape[1]], torch.tensor(lengths, dtype=torch.int32, device=DEV), dev_offsets(qo),
+                           max_q=max(news), scale=0.125, causal=causal, out=res[:, 1:n + 1, :D].transpose(0, 1))
+    au.close(lse, want, "lse")
+    au.close(out, want, "out")
+    assert (res[:, 0] == 7).all() and (res[:, -1] == 7).all() and (res[:, :, D:] == 7).all()
+
+
+@pytest.mark.parametrize("batch,Hk", [(65, 1), (9, 8), (7, 11), (300, 1)])
+def test_many_groups(batch, Hk):
+    """numbers of sequences and key heads that fill the rounds over the XCDs and that do not"""
+    g = torch.Generator().manual_seed(batch)
+    nq = torch.randint(0, 40, (batch,), generator=g).tolist()
+    nk = [x + y for x, y in zip(nq, torch.randint(0, 60, (batch,), generator=g).tolist())]
+    qo, ko = au.offsets(nq), au.offsets(nk)
+    q, k, v, do = (normal((n, h, 32), 20 + i, HF) for i, (n, h) in enumerate(((qo[-1], Hk), (ko[-1], Hk), (ko[-1], Hk), (qo[-1], Hk))))
+    want = au.batch(q, k, v, qo, ko, 0.2, dout=do)
+    how = dict(q_offsets=dev_offsets(qo), k_offsets=dev_offsets(ko), scale=float(np.float32(0.2)))
+    for most in (dict(max_q=max(nq), max_k=max(nk)), {}):         # the longest, and no more than that all rows may be one sequence's
+        out, lse = f3m.attention(q.to(DEV), k.to(DEV), v.to(DEV), **how, **most)
+        got = f3m.attention_grad(do.to(DEV), q.to(DEV), k.to(DEV), v.to(DEV), out, lse, **how, **most)
+        for name, x in zip(("out", "lse", "dq", "dk", "dv"), (out, lse) + got):
+            au.close(x, want, name)
