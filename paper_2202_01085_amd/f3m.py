@@ -442,7 +442,12 @@ def _no_graph(name, *tensors):
                 return
 
 
-def _attention_args(q, shape, rq, rk, rv, kv_heads, total_k, q_offsets, k_offsets, max_q, max_k, scale, causal, window, sinks):
+def _int32(x):
+    """x as the library's 32-bit integer: beyond it the largest, which is more than any length, or -1, which is refused as x would be"""
+    return max(-1, min(int(x), 2 ** 31 - 1))
+
+
+def _attention_args(q, shape, rq, rk, rv, kv_heads, total_k, room, q_offsets, k_offsets, max_q, max_k, scale, causal, window, sinks):
     rows, heads, dim = shape
     batch, qo = 1, None
     if q_offsets is not None:
@@ -451,8 +456,8 @@ def _attention_args(q, shape, rq, rk, rv, kv_heads, total_k, q_offsets, k_offset
     ko = None if k_offsets is None else _device_array(k_offsets, "k_offsets", torch.int32, q.device, (batch + 1,))
     if scale is None:
         scale = 1.0 / dim ** 0.5 if dim else 1.0
-    return AttentionArgs(DTYPES[q.dtype], batch, heads, kv_heads, dim, 1 if causal else 0, int(window), int(sinks), scale,
-                         rows if max_q is None else int(max_q), total_k if max_k is None else int(max_k), rows, total_k, qo, ko, rq, rk, rv)
+    return AttentionArgs(DTYPES[q.dtype], batch, heads, kv_heads, dim, 1 if causal else 0, _int32(window), _int32(sinks), scale,
+                         rows if max_q is None else min(_int32(max_q), rows), room if max_k is None else min(_int32(max_k), room), rows, total_k, qo, ko, rq, rk, rv)
 
 
 def _packed_args(q, k, v, q_offsets, k_offsets, max_q, max_k, scale, causal, window, sinks):
@@ -465,7 +470,7 @@ def _packed_args(q, k, v, q_offsets, k_offsets, max_q, max_k, scale, causal, win
     rv = _rows(v, "v", dtype, device, k.shape)
     if (q_offsets is None) != (k_offsets is None):
         raise ValueError("q_offsets and k_offsets are given both or neither")
-    return _attention_args(q, shape, rq, rk, rv, heads, rows, q_offsets, k_offsets, max_q, max_k, scale, causal, window, sinks)
+    return _attention_args(q, shape, rq, rk, rv, heads, rows, rows, q_offsets, k_offsets, max_q, max_k, scale, causal, window, sinks)
 
 
 def _lse(lse, shape, device, q=None):
@@ -636,7 +641,7 @@ class KVCache:
                 offsets = torch.arange(0, each * batch + 1, max(1, each), dtype=torch.int32, device=device) if each else \
                     torch.zeros(batch + 1, dtype=torch.int32, device=device)
                 most = each if most is None else most
-            a = _attention_args(q, shape, rq, Rows(), Rows(), c.kv_heads, 0, offsets, None, most, min(cols * c.page_size, 2 ** 31 - 65537) if max_k is None else max_k,
+            a = _attention_args(q, shape, rq, Rows(), Rows(), c.kv_heads, 0, min(cols * c.page_size, 2 ** 31 - 65537), offsets, None, most, max_k,
                                 scale, causal, window, sinks)
             if a.batch != batch:
                 raise ValueError("q_offsets must have one entry more than the table has rows")
