@@ -388,17 +388,23 @@ def direct_kmvm_xy_rows_f64(X, Y, b, lengthscale, rows, stream=None):
 _SIXTEEN = (torch.bfloat16, torch.float16)
 
 
-def _on_stream(device, stream, body):
+def _on_stream(device, stream, body, *tensors):
     """body(stream handle) with the tensors' device current and the call's stream the current one, so that what the binding allocates
-    belongs to it"""
-    if stream is None:
+    belongs to it.  A stream of the caller's holds the tensors that the call uses: their memory is not given to others before it is done."""
+    given = stream is not None
+    if not given:
         if device.index == torch.cuda.current_device():
             return body(torch._C._cuda_getCurrentRawStream(device.index))
         stream = torch.cuda.current_stream(device)
     elif stream.device != device:
         raise ValueError("the stream is of %s, the tensors are on %s" % (stream.device, device))
     with torch.cuda.stream(stream):
-        return body(stream.cuda_stream)
+        got = body(stream.cuda_stream)
+    if given:
+        for t in tensors:
+            if t is not None:
+                t.record_stream(stream)
+    return got
 
 
 def _rows(t, name, dtype=None, device=None, shape=None):
@@ -514,7 +520,7 @@ def attention(q, k, v, q_offsets=None, k_offsets=None, max_q=None, max_k=None, s
         _check(L.f3m_attention(ctypes.byref(a), ctypes.byref(to), ls.data_ptr() or None, at, need, handle))
         return o, ls
 
-    return _on_stream(device, stream, call)
+    return _on_stream(device, stream, call, q, k, v, q_offsets, k_offsets, out, lse)
 
 
 def attention_grad(dout, q, k, v, out, lse, q_offsets=None, k_offsets=None, max_q=None, max_k=None, scale=None, causal=True, window=0,
@@ -537,7 +543,7 @@ def attention_grad(dout, q, k, v, out, lse, q_offsets=None, k_offsets=None, max_
                                     ctypes.byref(to[1]), ctypes.byref(to[2]), at, need, handle))
         return tuple(got)
 
-    return _on_stream(device, stream, call)
+    return _on_stream(device, stream, call, dout, q, k, v, out, lse, q_offsets, k_offsets, dq, dk, dv)
 
 
 class KVCache:
@@ -596,7 +602,7 @@ class KVCache:
     def write(self, k, v, slots, stream=None):
         """f3m_cache_write: k, v (tokens, kv_heads, head_dim) to slots (tokens) int64, on the device; slots outside the cache are skipped.
         No slot may come twice in a call."""
-        _on_stream(self.k.device, stream, lambda handle: self._move(lib().f3m_cache_write, k, v, slots, handle))
+        _on_stream(self.k.device, stream, lambda handle: self._move(lib().f3m_cache_write, k, v, slots, handle), k, v, slots, *self._tensors)
 
     def read(self, slots, dtype=None, k=None, v=None, stream=None):
         """f3m_cache_read: (k, v) of the slots, of `dtype` (default: bfloat16 from an 8-bit cache, else the cache's); zeros for slots outside"""
@@ -609,7 +615,7 @@ class KVCache:
             self._move(lib().f3m_cache_read, kk, vv, slots, handle)
             return kk, vv
 
-        return _on_stream(self.k.device, stream, call)
+        return _on_stream(self.k.device, stream, call, k, v, slots, *self._tensors)
 
     def attention(self, q, table, lengths, q_offsets=None, max_q=None, max_k=None, scale=None, causal=True, window=0, sinks=0, out=None,
                   lse=None, stream=None):
@@ -654,4 +660,4 @@ class KVCache:
                                          ls.data_ptr() or None, at, need, handle))
             return o, ls
 
-        return _on_stream(device, stream, call)
+        return _on_stream(device, stream, call, q, table, lengths, q_offsets, out, lse, *self._tensors)

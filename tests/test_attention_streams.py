@@ -1,0 +1,68 @@
+"""Calls on a stream of the caller's: the tensors that a call uses are held until it is done."""
+import contextlib
+import types
+
+import pytest
+import torch
+
+from paper_2202_01085_amd import f3m
+
+
+class Tensor:
+    def __init__(self):
+        self.held = []
+
+    def record_stream(self, stream):
+        self.held.append(stream)
+
+
+def test_tensors_are_held_for_the_stream(monkeypatch):
+    monkeypatch.setattr(torch.cuda, "stream", lambda s: contextlib.nullcontext())
+    device = torch.device("cuda", 0)
+    stream = types.SimpleNamespace(device=device, cuda_stream=5)
+    x, y = Tensor(), Tensor()
+    assert f3m._on_stream(device, stream, lambda handle: handle, x, None, y) == 5
+    assert x.held == [stream] and y.held == [stream]
+    with pytest.raises(ValueError):
+        f3m._on_stream(torch.device("cuda", 1), stream, lambda handle: handle, x)
+
+
+@pytest.mark.gpu
+def test_inputs_freed_at_once_are_not_reused_before_the_call_is_done():
+    """a side stream kept busy, calls on it with tensors that nobody else holds, and new ones of the same sizes written meanwhile"""
+    dev, side = "cuda:0", torch.cuda.Stream()
+    g = torch.Generator(device=dev).manual_seed(1)
+    q, k = (torch.randn((2000, h, 64), generator=g, device=dev).bfloat16() for h in (4, 2))
+    off = torch.tensor([0, 700, 2000], dtype=torch.int32, device=dev)
+    want = f3m.attention(q, k, k, off, off)
+    wantg = f3m.attention_grad(q, q, k, k, *want, off, off)
+    c = f3m.KVCache.empty(125, 16, 2, 64, device=dev)
+    slots = torch.arange(2000, device=dev)
+    c.write(k, k, slots)
+    table, ln = torch.arange(125, dtype=torch.int32, device=dev)[None], torch.tensor([2000], dtype=torch.int32, device=dev)
+    wantc = c.attention(q[-3:], table, ln)
+    work = torch.randn((4096, 4096), device=dev)
+    torch.cuda.synchronize()
+    side.wait_stream(torch.cuda.current_stream())
+    with torch.cuda.stream(side):
+        for _ in range(20):
+            work = (work @ work).clamp(-1, 1)
+    fresh = lambda x: x.clone()      # noqa: E731
+    copies = [fresh(x) for x in (q, k, off)]
+    side.wait_stream(torch.cuda.current_stream())      # for the copies; the side stream is still at work
+    got = f3m.attention(copies[0], copies[1], copies[1], copies[2], copies[2], stream=side)
+    del copies
+    copies = [fresh(x) for x in (q, k, off, slots, table, ln)]
+    side.wait_stream(torch.cuda.current_stream())
+    gotg = f3m.attention_grad(copies[0], copies[0], copies[1], copies[1], *want, copies[2], copies[2], stream=side)
+    c2 = f3m.KVCache.empty(125, 16, 2, 64, device=dev)
+    side.wait_stream(torch.cuda.current_stream())
+    c2.write(copies[1], copies[1], copies[3], stream=side)
+    gotc = c2.attention(copies[0][-3:], copies[4], copies[5], stream=side)
+    del copies, c2
+    junk = [torch.full_like(x, 99) for x in (q, k, k, off, off, slots, table, ln) for _ in range(3)]
+    junk += [torch.full((125, 2, 16, 64), 99, dtype=torch.uint8, device=dev) for _ in range(6)]
+    torch.cuda.synchronize()
+    for a, b in zip(got + gotg + gotc, want + wantg + wantc):
+        assert torch.equal(a, b)
+    del junk
