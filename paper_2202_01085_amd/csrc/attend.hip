@@ -226,13 +226,16 @@ template <class T, int DP> struct Direct : Tile2<T, DP, KT> {
     }
 };
 
-// Many rows: a work item is 128 rows of one group, the four waves share tiles of 64 keys, two in LDS in turn.  Bound by the matrix cores
-// and by what LDS delivers to them (one operand of each product comes from there); at head size 64 by the exponentials, one for 256
-// multiply-adds, with 8-bit codes by their conversion.  Two blocks to a CU, so that one's exponentials run under the other's products: 16384
-// tokens with causal order, 8 heads of 128: 540 us, 1.02 PFLOP/s (a library's product of that size reaches 1.35), at a clock that the power
-// limit holds at 1.9 to 2.0 GHz.  A window of 1024 over four texts of up to 4099, 16 heads: 139 us.  10007 rows over 20000 keys, 4 heads of
-// 64: 280 us, 0.73 PFLOP/s.  1021 new tokens after up to 15000 in an 8-bit cache, window 4096: 165 us.  Tried without gain: two blocks of 32
-// rows to a wave, the products of one tile under the exponentials of another in one wave, eight waves in two groups in turn.
+// Many rows: a work item is 128 rows of one group, the four waves share tiles of 64 keys, two in LDS in turn.  Two blocks to a CU (three at a
+// head size of 64), so that one's exponentials run under the other's products.  No unit is full: matrix cores and vector issue (the
+// exponentials, one for 2 D multiply-adds, their sums, the mask) overlap in part only and fill about the whole time between them, at a clock that
+// the power limit holds below 2.4 GHz.  Shares of a launch's cycles, matrix cores / vector issue / LDS:
+//   16384 tokens with causal order, 8 heads of 128       502 to 536 us from card to card, 1.03 to 1.10 PFLOP/s    0.53 / 0.41 / 0.27 at 1.6 to 1.8 GHz
+//   10007 rows over 20000 keys, 4 heads of 64, fp16      270 us and 26 for the join, 0.76 PFLOP/s               0.38 / 0.58 / 0.19 at 1.9
+//   window of 1024, four texts of up to 4099, 16 heads   136 to 141 us; one wave to a SIMD, where two fit          0.23 / 0.23 / 0.11 at 2.2
+//   1021 new tokens after up to 15000 in 8 bits, window 4096   157 to 166 us; each block converts the codes     0.35 / 0.42 / 0.36 at 2.1
+// (a library's product of 16384^3 reaches 1.33 to 1.35 PFLOP/s on these cards).  Tried without gain: two blocks of 32 rows to a wave, the
+// products of one tile under the exponentials of another in one wave, eight waves in two groups in turn.
 template <class T, int DP, bool E8> __global__ __launch_bounds__(NT, DP == 128 ? 2 : 3) void attend_many(AttendArgs a) {
     using Row = Rows32<T, DP>;
     constexpr int ROWS = 128;
@@ -358,9 +361,9 @@ template <class T, int DP, bool E8> __global__ __launch_bounds__(NT, DP == 128 ?
 }
 
 // Few rows (single tokens, short chunks): a work item is 32 rows and a part of the keys; each of the four waves takes every fourth
-// tile of 32 keys through a ring in LDS of its own, and the four results are joined at the end.  Bound by the reading of K and V: a token each
-// of 64 sequences of up to 8192, 8 key heads of 128 in 8 bits: 136 us, 4.4 TB/s; one token after 131071 in 16 bits: 102 us with the join,
-// 5.3 TB/s (a copy reaches 4.7, reading and writing; some of it comes from the last-level cache).
+// tile of 32 keys through a ring in LDS of its own, and the four results are joined at the end.  Bound by the reading of K and V: one token after
+// 131071 in 16 bits: 102 us with the join, 5.3 TB/s where a copy, reading and writing, reaches 6.2; a token each of 64 sequences of up to 8192, 8
+// key heads of 128 in 8 bits: 136 us, 4.4 TB/s, since the sequences differ in length and the parts are cut by the longest.
 constexpr int PAGES_MAX = 1024;   // page numbers of a work item
 
 template <class T, int DP, bool E8> __global__ __launch_bounds__(NT, E8 ? 2 : 1) void attend_few(AttendArgs a) {
@@ -663,6 +666,8 @@ template <class T, int DP, bool E8> void launch(const AttendArgs &a, bool few, i
     }
 }
 
+// Head sizes in between run as the next of these: zeros in LDS and registers, and as many products.  At 80 and 96, as 128, that is 16 where 10 and
+// 12 would hold the values.
 template <class T> void launch_dim(const AttendArgs &a, bool e8, bool few, int64_t blocks, hipStream_t st) {
     if (a.dim <= 32) e8 ? launch<T, 32, true>(a, few, blocks, st) : launch<T, 32, false>(a, few, blocks, st);
     else if (a.dim <= 64) e8 ? launch<T, 64, true>(a, few, blocks, st) : launch<T, 64, false>(a, few, blocks, st);
@@ -677,12 +682,13 @@ template <class T> void launch_dim(const AttendArgs &a, bool e8, bool few, int64
 // them (one token after 131071 in 16 bits, 8 key heads: 112 us in 8 parts, 102 in 32, 109 in 64, 119 in 128; 16 sequences of 4096 in 8
 // bits: 55 us whole, 35 in 4 parts, 44 in 8).  Where that leaves one, three in 8 bits from 4096 keys on, since sequences differ in length (64
 // of up to 8192: 153 us whole, 137 in 3; all as long as the longest: 203 and 213; 64 of up to 1000: 28 and 43), in 16 bits it stays
-// (24 of up to 6000: 87 and 84; all as long: 106 and 132).
+// (24 of up to 6000: 87 and 84; all as long: 106 and 132; 64 of up to 8192: 249 and 234).
 // Up to 512 keys the second launch costs more than it saves.
 // attend_many: two blocks to a CU (three up to a head size of 64).  Where causal order makes the rows' lengths rise along the sequence, as many
 // parts as fill 88 % of those places, p parts of the longest being about (p + 1) / 2 to a tile (4096 tokens, 8 heads, one key head: 84 us
-// whole, 71 in 2 parts, 64 in 3, 80 in 4); else the fewest rounds for the work of one, a part costing some of it (twice 500 new tokens
-// after 7500, 8 heads, 2 key heads: 183 us whole, 67 in 4 parts, 63 in 8, 75 in 16).  Parts have 8 or 10 tiles or more, since shorter
+// whole, 71 in 2 parts, 64 in 3, 80 in 4); else the least time, counted in items: rounds of parts, and for each part that falls to a place
+// 0.02, its beginning, its end and its share of the join (twice 500 new tokens after 7500, 8 heads, 2 key heads: 183 us whole, 67 in 4
+// parts, 63 in 8, 75 in 16).  Parts have 8 or 10 tiles or more, since shorter
 // ones cost as much as they save (4 x 1024 tokens, 8 heads of 64, no order: 21 us whole, 33 in two parts).
 bool split(AttendArgs &a, int64_t max_k, bool e8) {
     const bool few = (int64_t)a.max_q * a.group <= 32;

@@ -7,9 +7,11 @@
 // P and dS are rounded to the inputs' type for the matrix cores.  fp16: P is held times 2^12; dS, whose size follows the loss, times
 // a power of two per kept row or key that goes down when a larger one comes, so both keep 11 bits.
 //
-// Bound by the matrix cores and LDS, at head size 64 by vector issue.  4 x 2048 tokens with causal order, 16 heads of 128, 4 key heads: rows
-// 119 us (0.87 PFLOP/s in three products), keys 172 (0.8 in four), sums of parts 8; 8192 tokens in a window of 1024, heads of 64: rows
-// 68, keys 118.
+// No unit is full: a SIMD has one to two waves, whose products, exponentials and LDS reads (one operand of each product, v too in grad_keys at
+// head sizes above 64) wait for one another.  Shares of a launch's cycles, matrix cores / vector issue / LDS:
+//   4 x 2048 tokens with causal order, 16 heads of 128, 4 key heads: rows 122 us 0.40 / 0.24 / 0.20, keys 173 us 0.36 / 0.21 / 0.28, sums of parts 9
+//   8192 tokens in a window of 1024, heads of 64:                    rows 71 us 0.31 / 0.34 / 0.16, keys 118 us 0.24 / 0.23 / 0.18, sums of parts 13
+// (three products a pair in the rows, four in the keys: 0.85 and 0.8 PFLOP/s in the first case).
 #include "attend.h"
 
 #include <algorithm>
@@ -570,8 +572,14 @@ int64_t sink_sums(const AttendArgs &a) { return a.sink_slots * a.sink_tiles * a.
 // How grad_keys is cut.  A block has a CU to itself at head sizes above 64, half of one below: 256 or 512 places.  Blocks go to the XCDs in
 // turn, whatever their length, so that a little more than one round of them takes as long as two.
 // With a window, without order or with few tokens after many keys, tiles are about equally long (`usual`) but those of the sinks, which
-// all later tokens see and which are always cut to the others' size.  There the parts are those of the shortest time by counting rounds
-// and steps, `ends` of them for a block's beginning and end and what the sum of the parts takes; a step is 2 us, 1 us up to 64.
+// all later tokens see and which are always cut to the others' size.  There the parts are those of the shortest time, counted in steps (a row tile
+// with a key tile; 2 us, 1 us up to a head size of 64): rounds of parts, each of them `ends` steps longer for its beginning and end, and the
+// join, (512 + n) / 128 us for n parts, up to 64 (512 + n) / 100 (512 parts at 128: 8.6 us).  All gradients, in us, by parts:
+//   8192 tokens, 16 heads, 4 key heads, window 1024      64: 167 whole, 157 in 2, 171 in 3, 165 in 4;  128: 263, 278, 295, 316
+//   the same at 64 with four sinks                       236, 216, 194, 197, in 6 206
+//   2000 tokens over 4000 keys, 4 heads, no order        64: 79, 70, 70, 68, in 6 75;  128: 107, 100, 117, 117
+//   512 new tokens after 7488, 8 heads, 2 key heads      64: 81, 71, 69, 68, in 6 78;  128: 106, 99, 118, 117
+// The rule takes 2, 1, 3, 4, 2, 4, 2.  It counts all of a batch as long as the longest: four of up to 4099, window 1024, four sinks 518, 494 in 2.
 // Else lengths fall to nothing along the keys, and p parts of the longest tile make (p + 1) / 2 to a tile: as many as fill 88 % of one
 // round or, if that is fewer than three, two, whose second ones are what others lack.  All gradients of 6709 tokens, 4 heads, one key
 // head: 692 us whole, 397 in 2 parts, 249 in 4, 202 in 6, 232 in 8; of 4 x 2048, 16 heads, 4 key heads: 322, 286 in 2, 296 in 3, 326 in 4.
