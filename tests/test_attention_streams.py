@@ -66,3 +66,57 @@ def test_inputs_freed_at_once_are_not_reused_before_the_call_is_done():
     for a, b in zip(got + gotg + gotc, want + wantg + wantc):
         assert torch.equal(a, b)
     del junk
+
+
+@pytest.mark.gpu
+def test_calls_captured_on_a_stream_that_is_given():
+    """stream= inside a capture on that stream, uneven lengths whose gradients go in parts and a paged call; every replay against the eager result"""
+    dev, side = "cuda:0", torch.cuda.Stream()
+    lengths = [1400, 3, 0, 700]
+    off = torch.tensor([0] + lengths, dtype=torch.int32).cumsum(0, dtype=torch.int32).to(dev)
+    n = sum(lengths)
+    q, k, do = (torch.zeros((n, h, 64), device=dev, dtype=torch.bfloat16) for h in (2, 1, 2))
+    how = dict(q_offsets=off, k_offsets=off, max_q=1400, max_k=1400, window=300, sinks=130)
+    c = f3m.KVCache.empty(132, 16, 1, 64, device=dev)
+    slots, table = torch.arange(n, device=dev), torch.arange(132, dtype=torch.int32, device=dev)[None]
+    ln, pages_q = torch.tensor([n], dtype=torch.int32, device=dev), torch.tensor([0, 40], dtype=torch.int32, device=dev)
+
+    def step(**more):
+        out, lse = f3m.attention(q, k, k, **how, **more)
+        grads = f3m.attention_grad(do, q, k, k, out, lse, **how, **more)
+        c.write(k, k, slots, **more)
+        return (out, lse) + grads + c.attention(q[:40], table, ln, pages_q, max_q=40, **more) + c.read(slots[:50], **more)
+
+    g = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(g, stream=side):
+        got = step(stream=side)
+    gen = torch.Generator(device=dev).manual_seed(2)
+    for _ in range(4):
+        for x in (q, k, do):
+            x.copy_(torch.randn(x.shape, generator=gen, device=dev))
+        want = step()
+        torch.cuda.synchronize()
+        for x in got:
+            x.fill_(7)
+        g.replay()
+        torch.cuda.synchronize()
+        assert all(torch.equal(a, b) for a, b in zip(got, want))
+
+
+@pytest.mark.gpu
+def test_calls_at_once_on_two_streams():
+    dev, streams = "cuda:0", [torch.cuda.Stream(), torch.cuda.Stream()]
+    gen = torch.Generator(device=dev).manual_seed(3)
+    sets = [[torch.randn((1500, h, 128), generator=gen, device=dev).bfloat16() for h in (1, 1, 1)] for _ in streams]
+    want = []
+    for q, k, v in sets:
+        out, lse = f3m.attention(q, k, v)
+        want.append((out, lse) + f3m.attention_grad(q, q, k, v, out, lse) + f3m.attention(q[:1], k, v))
+    torch.cuda.synchronize()
+    for _ in range(5):
+        got = [f3m.attention(*x, stream=s) for x, s in zip(sets, streams)]
+        grads = [f3m.attention_grad(x[0], *x, *y, stream=s) for x, y, s in zip(sets, got, streams)]
+        last = [f3m.attention(x[0][:1], *x[1:], stream=s) for x, s in zip(sets, streams)]
+        torch.cuda.synchronize()
+        for a, b, c, w in zip(got, grads, last, want):
+            assert all(torch.equal(x, y) for x, y in zip(a + b + c, w))
